@@ -397,6 +397,112 @@ int baseline_qkv_headnorm(void* y, int64_t M, int64_t ldy, int y_dtype, int64_t 
                           const int32_t* positions, const float* cos_tab, const float* sin_tab,
                           int64_t P, float q_scale, void* stream);
 
+/* ---- 4-bit weights ------------------------------------------------------------
+ * A weight in 4 bits: codes q = 0..15 with a scale and a zero point for each group of
+ * `group` consecutive k of a column (group = 32, 64 or 128; the last group of a column
+ * ends at K).  It stands for W4[k,n] = (q[k,n] - z[k/group,n]) s[k/group,n].  The scales
+ * are kept as fp32 of 12 significant bits, which hold every normal bf16 and fp16 value.
+ * Codes, scales and zero points live in one opaque buffer. */
+
+/* Bytes of the buffer for a logical [K, N] weight (N = 2F for FN_LAYOUT_GLU); 0 for
+ * invalid arguments and for buffers of 2^31 bytes or more.  Host only. */
+size_t fold_weights_w4_size(int64_t K, int64_t N, int layout, int group);
+
+/* Fold g into W (Prop. 1) and quantise, once, offline.  With w = g_k W[k,n], exactly:
+ *   zero_points = 0:  s = R(max |w| / 7), z = 8;
+ *   zero_points = 1:  lo = min(w, 0), hi = max(w, 0) over the group, s = R((hi - lo) / 15),
+ *                     z = clamp(rint(-lo / s), 0, 15);
+ *   q = clamp(rint(w / s) + z, 0, 15), quotients in fp64, ties to even; R rounds to 12
+ *   significant bits.  s below 2^-126 becomes 0 (then q = z = 8: the group stands for 0).
+ *   A group that holds a NaN or an infinity, or whose s exceeds fp32, stands for NaN.
+ * W, its strides, w_dtype and g as for fold_weights; W4 is 16-byte aligned and may overlap
+ * neither W nor g. */
+int fold_weights_w4(const void* W, int64_t stride_k, int64_t stride_n, int w_dtype, const float* g,
+                    int64_t K, int64_t N, int layout, int group, int zero_points, void* W4,
+                    void* stream);
+
+/* Pack a weight that is in 4 bits already (a checkpoint's), unchanged.
+ *   codes   [K, N] one code per byte, row stride ldc; the low 4 bits count.
+ *   scales  [ceil(K / group), N] fp32, row stride lds, rounded to 12 significant bits.
+ *   zeros   [ceil(K / group), N] zero points, row stride ldz, of which the low 6
+ *           bits count (0..63); NULL for 8 throughout.
+ * For FN_LAYOUT_GLU the columns are [gate | up].  No norm weight can be folded into codes:
+ * pass it to the products as g. */
+int pack_weights_w4(const uint8_t* codes, int64_t ldc, const float* scales, int64_t lds,
+                    const uint8_t* zeros, int64_t ldz, int64_t K, int64_t N, int layout, int group,
+                    void* W4, void* stream);
+
+/* The logical [K, N] weight that W4 stands for, in fp32 (exact), leading dimension
+ * ldo >= N.  Inspection and tests. */
+int unpack_weights_w4(const void* W4, int64_t K, int64_t N, int layout, int group, float* out,
+                      int64_t ldo, void* stream);
+
+/* flashnorm_linear, flashnorm_glu and rowscale_linear with a 4-bit weight.  The products run
+ * on the codes, unrounded; a group's sum is scaled in fp32.
+ *   a       [M, K] bf16 (fp32: FN_ERR_UNSUPPORTED), any M, K a multiple of 8.
+ *   g       optional [K] fp32 norm weight applied at run time, for a weight into which none
+ *           is folded.  a[m,k] g[k] enters the product as two bf16, its rounding and the rest:
+ *           2^-17 of it (flashnorm_linear_unfolded rounds it once, 2^-9).
+ *   W4      packed for K, N (2F for the GLU), the layout and `group`.
+ *   row_scale  optional [M] fp32; without it y = x W4 (a plain down projection).
+ * bias, inv_rms, outputs and errors as for the bf16-weight forms; no output may overlap an
+ * input (FN_ERR_ALIAS). */
+int flashnorm_linear_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype,
+                        const float* g, const void* W4, int64_t N, int group, float eps,
+                        const float* bias, void* y, int64_t ldy, int y_dtype, float* inv_rms,
+                        void* stream);
+int flashnorm_glu_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype, const float* g,
+                     const void* W4_gu, int64_t F, int group, float eps, void* out, int64_t ldo,
+                     int out_dtype, void* stream);
+int rowscale_linear_w4(const void* x, int64_t M, int64_t K, int64_t ldx, int x_dtype,
+                       const void* W4, int64_t N, int group, const float* row_scale, void* y,
+                       int64_t ldy, int y_dtype, void* stream);
+
+/* ---- Block residual -----------------------------------------------------------
+ * What joins a block's output x to the residual stream h and leads into the next block:
+ *   z      = x / sqrt(eps_post + mean(x^2)) * g_post        (z = x without g_post)
+ *   out    = res_scale h + branch_scale gate z              (no gate: 1)
+ *   normed = out / sqrt(eps_pre + mean(out^2)) * g_pre      (optional)
+ * computed in fp32 from the row as it was read, each output rounded once (normed from the
+ * unrounded sum).  A next projection that defers its norm needs `out` alone.
+ *   x, h    [M, K], dtype FN_F32 or FN_BF16 like every matrix here; K at most 16384
+ *           (FN_ERR_SIZE) and a multiple of 8 for bf16, 4 for fp32.
+ *   g_post, g_pre  optional [K] fp32, 16-byte aligned.
+ *   gate    optional [ceil(M / rows_per_gate), K]: row m takes gate row m / rows_per_gate
+ *           (1: a gate per token; the tokens of a sequence; M: one gate for all).
+ *   out     [M, K]; may be h itself (same pointer and leading dimension).
+ *   normed  optional [M, K], needs g_pre; may be x itself.
+ *   inv_rms optional [M] fp32: 1 / sqrt(eps_pre + mean(out^2)).
+ * Any other overlap of an output is FN_ERR_ALIAS. */
+int flashnorm_block_residual(const void* x, int64_t ldx, const void* h, int64_t ldh, int64_t M,
+                             int64_t K, int dtype, const float* g_post, float eps_post,
+                             const void* gate, int64_t ldg, int64_t rows_per_gate, float res_scale,
+                             float branch_scale, const float* g_pre, float eps_pre, void* out,
+                             int64_t ldo, void* normed, int64_t ldn, float* inv_rms, void* stream);
+
+/* Bytes of workspace that the backward pass may need for M rows; rows_per_gate = 0 without a
+ * gate.  0 for invalid arguments.  Host only. */
+size_t flashnorm_block_residual_bwd_size(int64_t M, int64_t K, int64_t rows_per_gate, int dtype);
+
+/* Gradients of the block residual.  x, h and the parameters are those of the forward call
+ * (h as it was before it), dh_out and dn the gradients at out and normed:
+ *   dx, dh   [M, K] (required).
+ *   dgate    optional, shaped like gate: summed over the rows that share a gate row.
+ *   dg_post, dg_pre  optional [K] fp32, summed over the rows.
+ *   dh_out   [M, K] or NULL for zeros; dn [M, K], required with g_pre and NULL without.
+ *   workspace  flashnorm_block_residual_bwd_size bytes, 16-byte aligned, written by the call.
+ * Sums over rows run in a fixed order.  With M = 0 the sums are zeros.  No output or
+ * workspace may overlap an input or another output. */
+int flashnorm_block_residual_bwd(const void* x, int64_t ldx, const void* h, int64_t ldh,
+                                 const void* dh_out, int64_t lddo, const void* dn, int64_t lddn,
+                                 int64_t M, int64_t K, int dtype, const float* g_post,
+                                 float eps_post, const void* gate, int64_t ldg,
+                                 int64_t rows_per_gate, float res_scale, float branch_scale,
+                                 const float* g_pre, float eps_pre, void* dx, int64_t lddx,
+                                 void* dh, int64_t lddh, void* dgate, int64_t lddg, float* dg_post,
+                                 float* dg_pre, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
 /* Human-readable name of a status code (static string; never NULL). */
 const char* flashnorm_status_string(int status);
 

@@ -7,6 +7,7 @@
 #include <mutex>
 
 #include "flashnorm.h"
+#include "fn_checks.h"
 #include "fn_launch.h"
 
 // The one piece of library-owned device memory: the workspace of
@@ -36,48 +37,6 @@ void* scratch_on_current_device() {
 }
 
 using fn::EpiArgs;
-
-constexpr int64_t kMaxLd = int64_t(1) << 21;    // leading dimensions, K (keeps tile extents < 2^31)
-constexpr int64_t kMaxRows = int64_t(1) << 30;  // M, N
-// Packed weight buffer: the matrix-core kernels address it with 32-bit byte
-// offsets and use offsets >= 2^31 as out-of-range (zero-returning) loads.
-constexpr int64_t kMaxPackedBytes = (int64_t(1) << 31) - 1;
-// Strides of the weight view fold_weights reads: with K <= 2^21 and N <= 2^30 every
-// element offset stays below 2^62.
-constexpr int64_t kMaxFoldStrideK = int64_t(1) << 40;
-constexpr int64_t kMaxFoldStrideN = int64_t(1) << 31;
-
-int64_t packed_bytes(int64_t K, int64_t N, bool glu, int64_t elem) {
-  return fn::packed_rows(K) * fn::packed_cols(N, glu) * elem;
-}
-
-bool dtype_ok(int d) { return d == FN_F32 || d == FN_BF16; }
-int64_t elem_size(int d) { return d == FN_BF16 ? 2 : 4; }
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-int64_t row_align(int d) { return 16 / elem_size(d); }
-
-bool overlaps(const void* p, int64_t pbytes, const void* q, int64_t qbytes) {
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(p), b0 = reinterpret_cast<uintptr_t>(q);
-  return a0 < b0 + (uintptr_t)qbytes && b0 < a0 + (uintptr_t)pbytes;
-}
-
-int64_t extent_bytes(int64_t rows, int64_t cols, int64_t ld, int dtype) {
-  return rows > 0 ? ((rows - 1) * ld + cols) * elem_size(dtype) : 0;
-}
-
-// Common checks of an activation-like operand [M, K] with leading dimension ld.
-int check_matrix(const void* p, int64_t M, int64_t K, int64_t ld, int dtype, bool required) {
-  if (M < 0 || K <= 0 || M > kMaxRows) return FN_ERR_SHAPE;
-  if (ld < K) return FN_ERR_SHAPE;
-  if (ld > kMaxLd) return FN_ERR_SIZE;
-  if (required && M > 0 && !p) return FN_ERR_NULL;
-  if (!aligned16(p) || ld % row_align(dtype)) return FN_ERR_ALIGN;
-  return FN_OK;
-}
-
-int check_eps(float eps) { return (isfinite(eps) && eps >= 0.0f) ? FN_OK : FN_ERR_VALUE; }
-
-int status_of(hipError_t e) { return e == hipSuccess ? FN_OK : FN_ERR_HIP; }
 
 struct OpDesc {
   const void* a;

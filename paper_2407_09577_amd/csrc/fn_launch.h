@@ -149,4 +149,69 @@ hipError_t launch_mla_latent_rows(void* y, int M, int ldy, int dtype, int L, int
                                   float eps_lat, const float* s_row, const int* pos, const float* cos_tab,
                                   const float* sin_tab, int P, hipStream_t stream);
 
+// 4-bit weights (fn_w4.h): codes, then the groups' scale words.
+inline int64_t w4_blocks(int64_t K) { return (K + 127) / 128; }
+inline int64_t w4_codes_bytes(int64_t K, int64_t N, int glu) { return w4_blocks(K) * 64 * packed_cols(N, glu); }
+inline int64_t w4_bytes(int64_t K, int64_t N, int glu, int group) {
+  return w4_codes_bytes(K, N, glu) + w4_blocks(K) * (128 / group) * packed_cols(N, glu) * 4;
+}
+inline unsigned* w4_scales(void* w4, int64_t K, int64_t N, int glu) {
+  return reinterpret_cast<unsigned*>(static_cast<char*>(w4) + w4_codes_bytes(K, N, glu));
+}
+struct W4FoldArgs {
+  const void* W;
+  int64_t sk, sn;
+  int w_dtype;
+  const float* g;
+  int64_t K, N;
+  int glu, group;
+  bool zero_points;
+  void* w4;
+  hipStream_t stream;
+};
+hipError_t launch_w4_fold(const W4FoldArgs& p);
+hipError_t launch_w4_pack(const uint8_t* codes, int64_t ldc, const float* scales, int64_t lds, const uint8_t* zeros,
+                          int64_t ldz, int64_t K, int64_t N, int glu, int group, void* w4, hipStream_t stream);
+hipError_t launch_w4_unpack(const void* w4, int64_t K, int64_t N, int glu, int group, float* out, int64_t ldo,
+                            hipStream_t stream);
+struct W4Args {
+  const __bf16* a;
+  int M, K, lda;
+  const void* codes;
+  const unsigned* scales;
+  int NP, KB, group;
+  int ncols;
+  __bf16* y;
+  int ldy;
+  int epi;
+  EpiArgs ep;  // ep.g_rt: run-time g, or nullptr
+  hipStream_t stream;
+};
+hipError_t launch_w4(const W4Args& p);
+
+// Block residual (residual.hip).
+struct ResidualArgs {
+  const void *x, *h, *gate;
+  int M, K, ldx, ldh, ldg, gate_rows;
+  int dtype;
+  const float *g_post, *g_pre;
+  float eps_post, eps_pre, res_scale, branch_scale;
+  // forward
+  void *out, *normed;
+  int ldo, ldn;
+  float* inv_rms;
+  // backward
+  const void *dh_out, *dn;
+  int lddo, lddn;
+  void *dx, *dh, *dgate;
+  int lddx, lddh, lddg;
+  float *dg_post, *dg_pre, *ws;
+  hipStream_t stream;
+};
+hipError_t launch_residual(const ResidualArgs& p);
+hipError_t launch_residual_bwd(const ResidualArgs& p);
+// fp32 values of partial sums that the backward pass holds in its workspace.
+int64_t residual_bwd_ws_floats(int64_t M, int64_t K, int64_t gate_rows, int dtype, bool post, bool pre, bool gate);
+constexpr int kResidualMaxK = 16384;
+
 }  // namespace fn

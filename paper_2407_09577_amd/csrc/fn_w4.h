@@ -1,0 +1,44 @@
+// 4-bit weights: the packed layout, shared by the folds and the products.
+//
+// A weight is held as codes q = 0..15 with, for each group of G = 32, 64 or 128 consecutive k of a
+// column, a scale s and a zero point z = 0..255: it stands for (q - z) s.  Packed columns are those
+// of fn_device.h (a GLU pairs gate and up blocks), padded to NP (a multiple of 16), and K is padded
+// to a multiple of 128.  The buffer holds
+//   codes   fragments of 1 KiB, k-block major: fragment (kb, cb) = 128 rows k x 16 columns at byte
+//           (kb * NP/16 + cb) * 1024; lane L = 16 c + p holds 16 bytes, word u the eight k =
+//           128 kb + 32 u + 8 c + e of column 16 cb + p: the operand of four matrix-core steps, so
+//           a wave loads a fragment with one 16-byte access per lane;
+//   scales  after the codes, one 32-bit word per group and packed column, [groups][NP] (groups of
+//           the padded K): the fp32 s rounded to 12 significant bits, which hold every bf16 and
+//           fp16 value, with z in the low byte.
+// Code e of a word is the nibble at bit 4 (e / 2) + 16 (e % 2): (word >> 4 i) & 0x000f000f are the
+// codes 2 i and 2 i + 1 in the halves of a register.  OR'ed with 0x4300 a half is the bf16 128 + q,
+// exactly; the products run on those, and the group's sum of the activations takes the 128 + z off:
+//   sum_k a (q - z) s = s (sum_k a (128 + q) - (128 + z) sum_k a).
+// One and-or per two weights this way, and no weight is rounded: the bf16 products are exact, the
+// sums are fp32.  The offset costs about 136/4 of a sum's last bits, 2^-18 of sum |a w|.
+#pragma once
+
+#include "fn_device.h"
+
+namespace fn {
+
+constexpr int kW4KB = 128;         // k extent of a code fragment
+constexpr unsigned kW4Bias = 128;  // added to every code by its bf16 form
+constexpr unsigned kW4ScaleMask = 0xfffff000u;
+
+// Bit of code e (0..7) in its word.
+__device__ __forceinline__ constexpr int w4_bit(int e) { return 4 * (e >> 1) + 16 * (e & 1); }
+
+// The eight codes of a word as bf16 128 + q, in k order.
+__device__ __forceinline__ bf16x8 w4_widen(unsigned w) {
+  u32x4 r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+  return __builtin_bit_cast(bf16x8, r);
+}
+
+__device__ __forceinline__ float w4_scale(unsigned word) { return __uint_as_float(word & kW4ScaleMask); }
+__device__ __forceinline__ float w4_zero(unsigned word) { return (float)(word & 0xffu); }
+
+}  // namespace fn

@@ -8,6 +8,7 @@ this module raises on first use -- there is no fallback.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import os
@@ -71,6 +72,18 @@ def _load():
         "baseline_mla_latent": ([P, I64, I64, I, I64, I64, P, F, P, P, P, I64, P], I),
         "flashnorm_linear_unfolded": ([P, I64, I64, I64, I, P, P, I64, F, P, P, I64, I, P, I, P], I),
         "flashnorm_glu_unfolded": ([P, I64, I64, I64, I, P, P, I64, F, P, I64, I, I, P], I),
+        "fold_weights_w4_size": ([I64, I64, I, I], ctypes.c_size_t),
+        "fold_weights_w4": ([P, I64, I64, I, P, I64, I64, I, I, I, P, P], I),
+        "pack_weights_w4": ([P, I64, P, I64, P, I64, I64, I64, I, I, P, P], I),
+        "unpack_weights_w4": ([P, I64, I64, I, I, P, I64, P], I),
+        "flashnorm_linear_w4": ([P, I64, I64, I64, I, P, P, I64, I, F, P, P, I64, I, P, P], I),
+        "flashnorm_glu_w4": ([P, I64, I64, I64, I, P, P, I64, I, F, P, I64, I, P], I),
+        "rowscale_linear_w4": ([P, I64, I64, I64, I, P, I64, I, P, P, I64, I, P], I),
+        "flashnorm_block_residual": ([P, I64, P, I64, I64, I64, I, P, F, P, I64, I64, F, F, P, F, P, I64, P, I64, P, P],
+                                     I),
+        "flashnorm_block_residual_bwd_size": ([I64, I64, I64, I], ctypes.c_size_t),
+        "flashnorm_block_residual_bwd": ([P, I64, P, I64, P, I64, P, I64, I64, I64, I, P, F, P, I64, I64, F, F, P, F, P,
+                                          I64, P, I64, P, I64, P, P, P, ctypes.c_size_t, P], I),
         "flashnorm_status_string": ([I], ctypes.c_char_p),
     }
     for name, (args, res) in sig.items():
@@ -519,3 +532,240 @@ def baseline_layernorm_linear(a, g, beta, W_packed, N, eps, x_ws=None, out=None,
                                              _ptr(y), _ld(y), path, _stream(stream)),
            "baseline_layernorm_linear")
     return y
+
+
+# The 4-bit weights and the block residual run on the GPU of their tensors, whatever the current one
+# is, and what they allocate belongs to the stream that works on it: a call for another GPU or stream
+# makes that one current and starts again.
+def _current_device():
+    return _raw_device() if _raw_device else torch.cuda.current_device()
+
+
+def _elsewhere(t, stream):
+    d = t.get_device()
+    return stream is not None or d < 0 or d != _current_device()
+
+
+@contextlib.contextmanager
+def _current(where, t, stream):
+    if not t.is_cuda:
+        raise ValueError(f"{where}: every tensor must be a GPU tensor (got one on {t.device})")
+    if stream is not None and not hasattr(stream, "cuda_stream"):
+        stream = torch.cuda.ExternalStream(int(stream), device=t.device)
+    if stream is not None and stream.device != t.device:
+        raise ValueError(f"{where}: a stream of {stream.device} and tensors on {t.device}")
+    with torch.cuda.device(t.device), torch.cuda.stream(stream):
+        yield
+
+
+def _on_gpu(where, t, *others):
+    """Every tensor on the GPU of the first (which is the current one)."""
+    dev = t.get_device()
+    for o in others:
+        if o is not None and o.get_device() != dev:
+            raise ValueError(f"{where}: tensors on {t.device} and {o.device}; all must be on one GPU")
+
+
+class W4Weight:
+    """A weight packed in 4 bits (fold_weights_w4, pack_weights_w4): the buffer and what it holds, a
+    logical [K, N] weight in groups of `group` k; N = 2F = [gate | up] for FN_LAYOUT_GLU."""
+    __slots__ = ("data", "K", "N", "layout", "group")
+
+    def __init__(self, data: torch.Tensor, K: int, N: int, layout: int, group: int):
+        need = _w4_bytes(K, N, layout, group)
+        if data.dtype != torch.uint8 or not data.is_contiguous() or data.numel() < need:
+            raise ValueError(f"a 4-bit weight of K = {K}, N = {N}, group {group} is {need} contiguous bytes")
+        self.data, self.K, self.N, self.layout, self.group = data, K, N, layout, group
+
+
+def _w4_bytes(K, N, layout, group):
+    need = _load().fold_weights_w4_size(K, N, layout, group)
+    if need == 0:
+        raise ValueError(f"no 4-bit weight of K = {K}, N = {N}, layout {layout}, group {group}")
+    return need
+
+
+def _new_w4(K, N, layout, group, device):
+    return W4Weight(torch.empty(_w4_bytes(K, N, layout, group), dtype=torch.uint8, device=device), K, N, layout, group)
+
+
+def fold_weights_w4(W: torch.Tensor, g=None, layout: int = FN_LAYOUT_LINEAR, group: int = 128,
+                    zero_points: bool = False, stream=None) -> W4Weight:
+    """Fold g into the logical [K, N] weight W (any strides; [Wg | Wu] for a GLU) and quantise it to
+    4 bits with one scale (and zero point) per column and `group` consecutive k."""
+    if _elsewhere(W, stream):
+        with _current("fold_weights_w4", W, stream):
+            return fold_weights_w4(W, g, layout, group, zero_points)
+    if W.dim() != 2:
+        raise ValueError("W must be a 2-D [K, N] tensor")
+    K, N = W.shape
+    _on_gpu("fold_weights_w4", W, g)
+    w4 = _new_w4(K, N, layout, group, W.device)
+    _check(_load().fold_weights_w4(_ptr(W), W.stride(0), W.stride(1), _dt(W), _ptr(_vec(g, K, "g")), K, N, layout, group,
+                                   int(bool(zero_points)), _ptr(w4.data), _stream(None)), "fold_weights_w4")
+    return w4
+
+
+def pack_weights_w4(codes: torch.Tensor, scales: torch.Tensor, zeros=None, layout: int = FN_LAYOUT_LINEAR,
+                    group: int = 128, stream=None) -> W4Weight:
+    """Pack codes [K, N] (uint8, 0..15) with scales [ceil(K / group), N] (bf16, fp16 or fp32) and zero
+    points of the same shape (uint8, 0..63; None: 8)."""
+    if _elsewhere(codes, stream):
+        with _current("pack_weights_w4", codes, stream):
+            return pack_weights_w4(codes, scales, zeros, layout, group)
+    if codes.dim() != 2 or codes.dtype != torch.uint8:
+        raise ValueError("codes must be a 2-D uint8 tensor")
+    K, N = codes.shape
+    w4 = _new_w4(K, N, layout, group, codes.device)
+    shape = (-(-K // group), N)
+    if scales.dtype not in (torch.float32, torch.bfloat16, torch.float16) or tuple(scales.shape) != shape:
+        raise ValueError(f"scales must be a floating-point {shape} tensor")
+    if zeros is not None and (zeros.dtype != torch.uint8 or tuple(zeros.shape) != shape):
+        raise ValueError(f"zeros must be a uint8 {shape} tensor")
+    _on_gpu("pack_weights_w4", codes, scales, zeros)
+    codes, scales = codes.contiguous(), scales.float().contiguous()
+    zeros = None if zeros is None else zeros.contiguous()
+    _check(_load().pack_weights_w4(_ptr(codes), N, _ptr(scales), N, _ptr(zeros), N, K, N, layout, group, _ptr(w4.data),
+                                   _stream(None)), "pack_weights_w4")
+    return w4
+
+
+def unpack_weights_w4(w4: W4Weight, stream=None) -> torch.Tensor:
+    """The logical [K, N] weight that w4 stands for, in fp32 (exact)."""
+    if _elsewhere(w4.data, stream):
+        with _current("unpack_weights_w4", w4.data, stream):
+            return unpack_weights_w4(w4)
+    out = torch.empty(w4.K, w4.N, dtype=torch.float32, device=w4.data.device)
+    _check(_load().unpack_weights_w4(_ptr(w4.data), w4.K, w4.N, w4.layout, w4.group, _ptr(out), w4.N, _stream(None)),
+           "unpack_weights_w4")
+    return out
+
+
+def _w4_args(where, a, w4, layout, N, out):
+    """Checks of a product's operands; returns M, K, the type code and the output."""
+    M, K = a.shape
+    if K != w4.K or layout != w4.layout:
+        raise ValueError(f"{where}: activations of width {K}, layout {layout}, and a 4-bit weight of K = {w4.K}, "
+                         f"layout {w4.layout}")
+    code = _dt(a)
+    if out is None:
+        out = _new_out(M, N, a)
+    elif out.dtype != a.dtype or tuple(out.shape) != (M, N):
+        raise ValueError(f"{where}: output of shape {tuple(out.shape)}, {out.dtype}, expected ({M}, {N}), {a.dtype}")
+    return M, K, code, out
+
+
+def flashnorm_linear_w4(a: torch.Tensor, w4: W4Weight, eps: float, g=None, bias=None, out=None, inv_rms=None,
+                        stream=None) -> torch.Tensor:
+    """y = RMSNorm(a) W4 (+ bias), deferred; g: the norm weight, where it is not folded into w4."""
+    if _elsewhere(a, stream):
+        with _current("flashnorm_linear_w4", a, stream):
+            return flashnorm_linear_w4(a, w4, eps, g, bias, out, inv_rms)
+    N = w4.N
+    M, K, code, y = _w4_args("flashnorm_linear_w4", a, w4, FN_LAYOUT_LINEAR, N, out)
+    _on_gpu("flashnorm_linear_w4", a, w4.data, y, g, bias, inv_rms)
+    _check(_load().flashnorm_linear_w4(a.data_ptr(), M, K, _ld(a), code, _ptr(_vec(g, K, "g")), w4.data.data_ptr(), N,
+                                       w4.group, eps, _ptr(_vec(bias, N, "bias")), y.data_ptr(), _ld(y), code,
+                                       _ptr(_vec(inv_rms, M, "inv_rms")), _stream(None)), "flashnorm_linear_w4")
+    return y
+
+
+def flashnorm_glu_w4(a: torch.Tensor, w4: W4Weight, eps: float, g=None, out=None, stream=None) -> torch.Tensor:
+    """silu(RMSNorm(a) Wg) * (RMSNorm(a) Wu) with w4 = [Wg | Wu] (FN_LAYOUT_GLU)."""
+    if _elsewhere(a, stream):
+        with _current("flashnorm_glu_w4", a, stream):
+            return flashnorm_glu_w4(a, w4, eps, g, out)
+    F = w4.N // 2
+    M, K, code, o = _w4_args("flashnorm_glu_w4", a, w4, FN_LAYOUT_GLU, F, out)
+    _on_gpu("flashnorm_glu_w4", a, w4.data, o, g)
+    _check(_load().flashnorm_glu_w4(a.data_ptr(), M, K, _ld(a), code, _ptr(_vec(g, K, "g")), w4.data.data_ptr(), F,
+                                    w4.group, eps, o.data_ptr(), _ld(o), code, _stream(None)), "flashnorm_glu_w4")
+    return o
+
+
+def rowscale_linear_w4(x: torch.Tensor, w4: W4Weight, row_scale=None, out=None, stream=None) -> torch.Tensor:
+    """y = (x W4) * row_scale[m], or x W4: a down projection, with a deferred norm's scale or without."""
+    if _elsewhere(x, stream):
+        with _current("rowscale_linear_w4", x, stream):
+            return rowscale_linear_w4(x, w4, row_scale, out)
+    N = w4.N
+    M, K, code, y = _w4_args("rowscale_linear_w4", x, w4, FN_LAYOUT_LINEAR, N, out)
+    _on_gpu("rowscale_linear_w4", x, w4.data, y, row_scale)
+    _check(_load().rowscale_linear_w4(x.data_ptr(), M, K, _ld(x), code, w4.data.data_ptr(), N, w4.group,
+                                      _ptr(_vec(row_scale, M, "row_scale")), y.data_ptr(), _ld(y), code, _stream(None)),
+           "rowscale_linear_w4")
+    return y
+
+
+def _residual_args(where, x, h, gate, rows_per_gate, *others):
+    """Checks of the block residual's matrices: one shape and type, and the gate's rows."""
+    M, K = shape = x.shape
+    dtype = x.dtype
+    code = _dt(x)
+    for t in (h, *others):
+        if t is not None and (t.shape != shape or t.dtype != dtype):
+            raise ValueError(f"{where}: a tensor of shape {tuple(t.shape)}, {t.dtype}, beside {tuple(shape)}, {dtype}")
+    if gate is not None:
+        if rows_per_gate < 1:
+            raise ValueError(f"{where}: rows_per_gate must be at least 1")
+        B = -(-M // rows_per_gate)
+        if tuple(gate.shape) != (B, K) or gate.dtype != dtype:
+            raise ValueError(f"{where}: a gate of shape {tuple(gate.shape)}, {gate.dtype}; {M} rows, {rows_per_gate} to a "
+                             f"gate, need ({B}, {K}), {dtype}")
+    return M, K, code
+
+
+def _opt_ld(t):
+    return 0 if t is None else _ld(t)
+
+
+def flashnorm_block_residual(x: torch.Tensor, h: torch.Tensor, g_post=None, eps_post: float = 0.0, gate=None,
+                             rows_per_gate: int = 1, res_scale: float = 1.0, branch_scale: float = 1.0, g_pre=None,
+                             eps_pre: float = 0.0, out=None, normed=None, inv_rms=None, stream=None):
+    """out = res_scale h + branch_scale gate RMSNorm(x; g_post), normed = RMSNorm(out; g_pre).  Returns
+    (out, normed); normed is None without g_pre.  out may be h, normed may be x."""
+    where = "flashnorm_block_residual"
+    if _elsewhere(x, stream):
+        with _current(where, x, stream):
+            return flashnorm_block_residual(x, h, g_post, eps_post, gate, rows_per_gate, res_scale, branch_scale, g_pre,
+                                            eps_pre, out, normed, inv_rms)
+    M, K, code = _residual_args(where, x, h, gate, rows_per_gate, out, normed)
+    if normed is not None and g_pre is None:
+        raise ValueError(f"{where}: normed needs g_pre")
+    if out is None:
+        out = _new_out(M, K, x)
+    if normed is None and g_pre is not None:
+        normed = _new_out(M, K, x)
+    _on_gpu(where, x, h, g_post, gate, g_pre, out, normed, inv_rms)
+    _check(_load().flashnorm_block_residual(
+        x.data_ptr(), _ld(x), h.data_ptr(), _ld(h), M, K, code, _ptr(_vec(g_post, K, "g_post")), eps_post, _ptr(gate),
+        _opt_ld(gate), rows_per_gate, res_scale, branch_scale, _ptr(_vec(g_pre, K, "g_pre")), eps_pre, out.data_ptr(),
+        _ld(out), _ptr(normed), _opt_ld(normed), _ptr(_vec(inv_rms, M, "inv_rms")), _stream(None)), where)
+    return out, normed
+
+
+def flashnorm_block_residual_bwd(x: torch.Tensor, h: torch.Tensor, dh_out, dn=None, g_post=None, eps_post: float = 0.0,
+                                 gate=None, rows_per_gate: int = 1, res_scale: float = 1.0, branch_scale: float = 1.0,
+                                 g_pre=None, eps_pre: float = 0.0, stream=None):
+    """Gradients of flashnorm_block_residual from those at out (dh_out, None: zeros) and normed (dn, with
+    g_pre).  Returns (dx, dh, dgate, dg_post, dg_pre), None for what the call has not."""
+    where = "flashnorm_block_residual_bwd"
+    if _elsewhere(x, stream):
+        with _current(where, x, stream):
+            return flashnorm_block_residual_bwd(x, h, dh_out, dn, g_post, eps_post, gate, rows_per_gate, res_scale,
+                                                branch_scale, g_pre, eps_pre)
+    M, K, code = _residual_args(where, x, h, gate, rows_per_gate, dh_out, dn)
+    _on_gpu(where, x, h, dh_out, dn, g_post, gate, g_pre)
+    lib = _load()
+    need = lib.flashnorm_block_residual_bwd_size(M, K, 0 if gate is None else rows_per_gate, code)
+    dx, dh = _new_out(M, K, x), _new_out(M, K, x)
+    dgate = None if gate is None else _new_out(gate.shape[0], K, x)
+    dpost = None if g_post is None else torch.empty(K, dtype=torch.float32, device=x.device)
+    dpre = None if g_pre is None else torch.empty(K, dtype=torch.float32, device=x.device)
+    ws = torch.empty(need, dtype=torch.uint8, device=x.device)
+    _check(lib.flashnorm_block_residual_bwd(
+        x.data_ptr(), _ld(x), h.data_ptr(), _ld(h), _ptr(dh_out), _opt_ld(dh_out), _ptr(dn), _opt_ld(dn), M, K, code,
+        _ptr(_vec(g_post, K, "g_post")), eps_post, _ptr(gate), _opt_ld(gate), rows_per_gate, res_scale, branch_scale,
+        _ptr(_vec(g_pre, K, "g_pre")), eps_pre, dx.data_ptr(), _ld(dx), dh.data_ptr(), _ld(dh), _ptr(dgate),
+        _opt_ld(dgate), _ptr(dpost), _ptr(dpre), ws.data_ptr(), need, _stream(None)), where)
+    return dx, dh, dgate, dpost, dpre
