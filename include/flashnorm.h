@@ -437,26 +437,35 @@ int pack_weights_w4(const uint8_t* codes, int64_t ldc, const float* scales, int6
 int unpack_weights_w4(const void* W4, int64_t K, int64_t N, int layout, int group, float* out,
                       int64_t ldo, void* stream);
 
-/* flashnorm_linear, flashnorm_glu and rowscale_linear with a 4-bit weight.  The products run
- * on the codes, unrounded; a group's sum is scaled in fp32.
+/* Bytes of workspace that a product of M rows with a logical [K, N] weight of the layout needs
+ * (0 for few rows, and for invalid arguments).  Host only. */
+size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout);
+
+/* flashnorm_linear, flashnorm_glu and rowscale_linear with a 4-bit weight.  Sums are fp32.  Few
+ * rows multiply the codes unrounded and scale a group's sum; many rows multiply a weight that is
+ * rounded to 11 bits (at most 2^-11 of it, with its scale's rounding).  Which way a call goes
+ * depends on M, K, N and the layout alone.
  *   a       [M, K] bf16 (fp32: FN_ERR_UNSUPPORTED), any M, K a multiple of 8.
  *   g       optional [K] fp32 norm weight applied at run time, for a weight into which none
- *           is folded.  a[m,k] g[k] enters the product as two bf16, its rounding and the rest:
- *           2^-17 of it (flashnorm_linear_unfolded rounds it once, 2^-9).
+ *           is folded.  a[m,k] g[k] enters the product with 11 bits or more (flashnorm_linear_unfolded
+ *           rounds it to 8).
  *   W4      packed for K, N (2F for the GLU), the layout and `group`.
  *   row_scale  optional [M] fp32; without it y = x W4 (a plain down projection).
+ *   workspace  flashnorm_w4_workspace_size bytes, 16-byte aligned, written by the call; one
+ *           workspace serves calls that follow each other on a stream (FN_ERR_SIZE where it is
+ *           too small, FN_ERR_NULL where it is needed and missing).
  * bias, inv_rms, outputs and errors as for the bf16-weight forms; no output may overlap an
- * input (FN_ERR_ALIAS). */
+ * input or another output (FN_ERR_ALIAS).  A row of a that holds a NaN or an infinity gives NaN. */
 int flashnorm_linear_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype,
                         const float* g, const void* W4, int64_t N, int group, float eps,
                         const float* bias, void* y, int64_t ldy, int y_dtype, float* inv_rms,
-                        void* stream);
+                        void* workspace, size_t workspace_bytes, void* stream);
 int flashnorm_glu_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype, const float* g,
                      const void* W4_gu, int64_t F, int group, float eps, void* out, int64_t ldo,
-                     int out_dtype, void* stream);
+                     int out_dtype, void* workspace, size_t workspace_bytes, void* stream);
 int rowscale_linear_w4(const void* x, int64_t M, int64_t K, int64_t ldx, int x_dtype,
                        const void* W4, int64_t N, int group, const float* row_scale, void* y,
-                       int64_t ldy, int y_dtype, void* stream);
+                       int64_t ldy, int y_dtype, void* workspace, size_t workspace_bytes, void* stream);
 
 /* ---- Block residual -----------------------------------------------------------
  * What joins a block's output x to the residual stream h and leads into the next block:

@@ -39,6 +39,8 @@ struct W4Op {
   const float* bias;
   float* inv_rms;
   const float* row_scale;
+  void* ws;
+  size_t ws_bytes;
   void* stream;
 };
 
@@ -71,6 +73,18 @@ int run_w4(const W4Op& d) {
         (d.bias && overlaps(d.inv_rms, rbytes, d.bias, d.ncols * 4)))
       return FN_ERR_ALIAS;
   }
+  const int64_t NP = fn::packed_cols(N, d.glu), need = fn::w4_workspace(d.M, d.K, NP, d.glu);
+  if (need > 0) {
+    if (!d.ws) return FN_ERR_NULL;
+    if (!aligned16(d.ws)) return FN_ERR_ALIGN;
+    if ((uint64_t)need > d.ws_bytes) return FN_ERR_SIZE;
+    if (overlaps(d.ws, need, d.y, ybytes) || overlaps(d.ws, need, d.a, extent_bytes(d.M, d.K, d.lda, d.a_dtype)) ||
+        overlaps(d.ws, need, d.w4, wbytes) || (d.g && overlaps(d.ws, need, d.g, d.K * 4)) ||
+        (d.bias && overlaps(d.ws, need, d.bias, d.ncols * 4)) ||
+        (d.row_scale && overlaps(d.ws, need, d.row_scale, d.M * 4)) ||
+        (d.inv_rms && overlaps(d.ws, need, d.inv_rms, d.M * 4)))
+      return FN_ERR_ALIAS;
+  }
   EpiArgs ep{};
   ep.eps = d.eps;
   ep.inv_k = 1.0f / (float)d.K;
@@ -80,9 +94,9 @@ int run_w4(const W4Op& d) {
   ep.row_scale = d.row_scale;
   ep.g_rt = d.g;
   fn::W4Args p{(const __bf16*)d.a, (int)d.M, (int)d.K, (int)d.lda, d.w4,
-               fn::w4_scales(const_cast<void*>(d.w4), d.K, N, d.glu), (int)fn::packed_cols(N, d.glu),
-               (int)fn::w4_blocks(d.K), d.group, (int)d.ncols, (__bf16*)d.y, (int)d.ldy, d.epi, ep,
-               (hipStream_t)d.stream};
+               fn::w4_scales(const_cast<void*>(d.w4), d.K, N, d.glu),
+               fn::w4_norms(const_cast<void*>(d.w4), d.K, N, d.glu, d.group), (int)NP, (int)fn::w4_blocks(d.K), d.group,
+               (int)d.ncols, (__bf16*)d.y, (int)d.ldy, d.epi, ep, d.ws, (hipStream_t)d.stream};
   const hipError_t e = fn::launch_w4(p);
   return e == hipErrorInvalidConfiguration ? FN_ERR_SIZE : status_of(e);
 }
@@ -142,23 +156,29 @@ int unpack_weights_w4(const void* W4, int64_t K, int64_t N, int layout, int grou
   return status_of(fn::launch_w4_unpack(W4, K, N, layout == FN_LAYOUT_GLU, group, out, ldo, (hipStream_t)stream));
 }
 
+size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout) {
+  if (M < 0 || M > kMaxRows || check_w4(K, N, layout, 128)) return 0;
+  const bool glu = layout == FN_LAYOUT_GLU;
+  return (size_t)fn::w4_workspace(M, K, fn::packed_cols(N, glu), glu);
+}
+
 int flashnorm_linear_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype, const float* g, const void* W4,
                         int64_t N, int group, float eps, const float* bias, void* y, int64_t ldy, int y_dtype,
-                        float* inv_rms, void* stream) {
+                        float* inv_rms, void* workspace, size_t workspace_bytes, void* stream) {
   return run_w4(W4Op{a, M, K, lda, a_dtype, g, W4, N, 0, group, y, ldy, y_dtype, fn::EPI_RMS, eps, bias, inv_rms,
-                     nullptr, stream});
+                     nullptr, workspace, workspace_bytes, stream});
 }
 
 int flashnorm_glu_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype, const float* g, const void* W4_gu,
-                     int64_t F, int group, float eps, void* out, int64_t ldo, int out_dtype, void* stream) {
+                     int64_t F, int group, float eps, void* out, int64_t ldo, int out_dtype, void* workspace, size_t workspace_bytes, void* stream) {
   return run_w4(W4Op{a, M, K, lda, a_dtype, g, W4_gu, F, 1, group, out, ldo, out_dtype, fn::EPI_GLU, eps, nullptr,
-                     nullptr, nullptr, stream});
+                     nullptr, nullptr, workspace, workspace_bytes, stream});
 }
 
 int rowscale_linear_w4(const void* x, int64_t M, int64_t K, int64_t ldx, int x_dtype, const void* W4, int64_t N,
-                       int group, const float* row_scale, void* y, int64_t ldy, int y_dtype, void* stream) {
+                       int group, const float* row_scale, void* y, int64_t ldy, int y_dtype, void* workspace, size_t workspace_bytes, void* stream) {
   return run_w4(W4Op{x, M, K, ldx, x_dtype, nullptr, W4, N, 0, group, y, ldy, y_dtype, fn::EPI_ROWSCALE, 0.0f, nullptr,
-                     nullptr, row_scale, stream});
+                     nullptr, row_scale, workspace, workspace_bytes, stream});
 }
 
 }  // extern "C"

@@ -149,14 +149,17 @@ hipError_t launch_mla_latent_rows(void* y, int M, int ldy, int dtype, int L, int
                                   float eps_lat, const float* s_row, const int* pos, const float* cos_tab,
                                   const float* sin_tab, int P, hipStream_t stream);
 
-// 4-bit weights (fn_w4.h): codes, then the groups' scale words.
+// 4-bit weights (fn_w4.h): codes, the groups' scale words, the columns' powers of two.
 inline int64_t w4_blocks(int64_t K) { return (K + 127) / 128; }
 inline int64_t w4_codes_bytes(int64_t K, int64_t N, int glu) { return w4_blocks(K) * 64 * packed_cols(N, glu); }
 inline int64_t w4_bytes(int64_t K, int64_t N, int glu, int group) {
-  return w4_codes_bytes(K, N, glu) + w4_blocks(K) * (128 / group) * packed_cols(N, glu) * 4;
+  return w4_codes_bytes(K, N, glu) + (w4_blocks(K) * (128 / group) + 1) * packed_cols(N, glu) * 4;
 }
 inline unsigned* w4_scales(void* w4, int64_t K, int64_t N, int glu) {
   return reinterpret_cast<unsigned*>(static_cast<char*>(w4) + w4_codes_bytes(K, N, glu));
+}
+inline float* w4_norms(void* w4, int64_t K, int64_t N, int glu, int group) {
+  return reinterpret_cast<float*>(static_cast<char*>(w4) + w4_bytes(K, N, glu, group)) - packed_cols(N, glu);
 }
 struct W4FoldArgs {
   const void* W;
@@ -179,15 +182,19 @@ struct W4Args {
   int M, K, lda;
   const void* codes;
   const unsigned* scales;
+  const float* norms;
   int NP, KB, group;
   int ncols;
   __bf16* y;
   int ldy;
   int epi;
   EpiArgs ep;  // ep.g_rt: run-time g, or nullptr
+  void* ws;    // w4_workspace bytes
   hipStream_t stream;
 };
+// hipErrorInvalidConfiguration: more workgroups than a launch takes.
 hipError_t launch_w4(const W4Args& p);
+int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu);
 
 // Block residual (residual.hip).
 struct ResidualArgs {

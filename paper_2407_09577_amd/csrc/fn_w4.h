@@ -1,7 +1,7 @@
 // 4-bit weights: the packed layout, shared by the folds and the products.
 //
 // A weight is held as codes q = 0..15 with, for each group of G = 32, 64 or 128 consecutive k of a
-// column, a scale s and a zero point z = 0..255: it stands for (q - z) s.  Packed columns are those
+// column, a scale s and a zero point z = 0..63: it stands for (q - z) s.  Packed columns are those
 // of fn_device.h (a GLU pairs gate and up blocks), padded to NP (a multiple of 16), and K is padded
 // to a multiple of 128.  The buffer holds
 //   codes   fragments of 1 KiB, k-block major: fragment (kb, cb) = 128 rows k x 16 columns at byte
@@ -10,13 +10,21 @@
 //           a wave loads a fragment with one 16-byte access per lane;
 //   scales  after the codes, one 32-bit word per group and packed column, [groups][NP] (groups of
 //           the padded K): the fp32 s rounded to 12 significant bits, which hold every bf16 and
-//           fp16 value, with z in the low byte.
+//           fp16 value, with z in the low six.
+//   norms   after the scales, an fp32 power of two per packed column, [NP]: what brings the column's
+//           largest |s| into [2^9, 2^10), for the many-row kernel's fp16 weights.
 // Code e of a word is the nibble at bit 4 (e / 2) + 16 (e % 2): (word >> 4 i) & 0x000f000f are the
-// codes 2 i and 2 i + 1 in the halves of a register.  OR'ed with 0x4300 a half is the bf16 128 + q,
-// exactly; the products run on those, and the group's sum of the activations takes the 128 + z off:
+// codes 2 i and 2 i + 1 in the halves of a register, and one and-or makes two weights of them.
+//
+// Few rows: OR'ed with 0x4300 a half is the bf16 128 + q, exactly, and the group's sum of the
+// activations takes the 128 + z off again:
 //   sum_k a (q - z) s = s (sum_k a (128 + q) - (128 + z) sum_k a).
-// One and-or per two weights this way, and no weight is rounded: the bf16 products are exact, the
-// sums are fp32.  The offset costs about 136/4 of a sum's last bits, 2^-18 of sum |a w|.
+// No weight is rounded: the bf16 products are exact, the sums are fp32.  The offset costs last bits of
+// the sums, 2^-18 of sum |a w|.
+// Many rows: OR'ed with 0x6400 a half is the fp16 1024 + q; less 1024 + z, times the scale as fp16, it is
+// the weight in eleven bits (w4_kernels.h).
+// The products run with the activations as the matrix cores' first operand, so a lane's four results
+// are four rows of one column, whose scale word is the one that its codes need too.
 #pragma once
 
 #include "fn_device.h"
@@ -24,7 +32,7 @@
 namespace fn {
 
 constexpr int kW4KB = 128;         // k extent of a code fragment
-constexpr unsigned kW4Bias = 128;  // added to every code by its bf16 form
+constexpr float kW4Bias = 128.0f;  // added to every code by its bf16 form
 constexpr unsigned kW4ScaleMask = 0xfffff000u;
 
 // Bit of code e (0..7) in its word.
@@ -39,6 +47,6 @@ __device__ __forceinline__ bf16x8 w4_widen(unsigned w) {
 }
 
 __device__ __forceinline__ float w4_scale(unsigned word) { return __uint_as_float(word & kW4ScaleMask); }
-__device__ __forceinline__ float w4_zero(unsigned word) { return (float)(word & 0xffu); }
+__device__ __forceinline__ float w4_zero(unsigned word) { return (float)(word & 63u); }
 
 }  // namespace fn

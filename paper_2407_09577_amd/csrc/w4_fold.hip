@@ -110,6 +110,31 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t* __restrict_
   scales[grp * NPB * 16 + cb * 16 + (lane & 15)] = word;
 }
 
+// The power of two that brings a packed column's largest |s| into [2^9, 2^10): sixteen threads per column.
+__global__ __launch_bounds__(256) void w4_norms_kernel(const unsigned* __restrict__ scales, int64_t groups, int64_t NP,
+                                                       float* __restrict__ norms) {
+  __shared__ unsigned red[16][16];
+  const int c = threadIdx.x & 15, w = threadIdx.x >> 4;
+  const int64_t col = (int64_t)blockIdx.x * 16 + c;
+  unsigned top = 0;
+#pragma unroll 4
+  for (int64_t g = w; g < groups; g += 16) top = max(top, scales[g * NP + col] & 0x7ffff000u);
+  red[w][c] = top;
+  __syncthreads();
+  if (w) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) top = max(top, red[i][c]);
+  const unsigned ex = top >> 23;  // 255: a column that holds no finite scale stays as it is
+  norms[col] = ex == 255u || top == 0u ? 1.0f : __uint_as_float(min(263u - ex, 254u) << 23);
+}
+
+static hipError_t launch_w4_norms(void* w4, int64_t K, int64_t N, int glu, int group, hipStream_t stream) {
+  const int64_t NP = packed_cols(N, glu);
+  hipLaunchKernelGGL(w4_norms_kernel, dim3((unsigned)(NP / 16)), dim3(256), 0, stream, w4_scales(w4, K, N, glu),
+                     w4_blocks(K) * (128 / group), NP, w4_norms(w4, K, N, glu, group));
+  return hipGetLastError();
+}
+
 // The weight that the codes stand for, in fp32 (exact: (q - z) has 9 bits, s 12).
 __global__ __launch_bounds__(256) void w4_unpack_kernel(const u32x4* __restrict__ codes,
                                                         const unsigned* __restrict__ scales, int64_t K, int64_t N,
@@ -144,7 +169,8 @@ static hipError_t launch_w4_fold_t(const W4FoldArgs& p) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)kgroups * ((NPB + cstep - 1) / cstep)), dim3(256), 0, p.stream, W, p.sk,
                        p.sn, p.K, p.N, p.g, p.glu, vec, aligned(p.g), p.zero_points, NPB, KB, kgroups,
                        reinterpret_cast<u32x4*>(p.w4), w4_scales(p.w4, p.K, p.N, p.glu));
-    return hipGetLastError();
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess ? launch_w4_norms(p.w4, p.K, p.N, p.glu, p.group, p.stream) : e;
   };
   return p.group == 32 ? go(w4_fold_kernel<T, 1>) : p.group == 64 ? go(w4_fold_kernel<T, 2>) : go(w4_fold_kernel<T, 4>);
 }
@@ -158,7 +184,8 @@ hipError_t launch_w4_pack(const uint8_t* codes, int64_t ldc, const float* scales
   const int NPB = (int)(packed_cols(N, glu) / 16), KB = (int)w4_blocks(K);
   hipLaunchKernelGGL(w4_pack_kernel, dim3((unsigned)KB * ((NPB + 3) / 4)), dim3(256), 0, stream, codes, ldc, scales, lds,
                      zeros, ldz, K, N, glu, group / 32, NPB, KB, reinterpret_cast<u32x4*>(w4), w4_scales(w4, K, N, glu));
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? launch_w4_norms(w4, K, N, glu, group, stream) : e;
 }
 
 hipError_t launch_w4_unpack(const void* w4, int64_t K, int64_t N, int glu, int group, float* out, int64_t ldo,

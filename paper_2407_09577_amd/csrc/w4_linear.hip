@@ -1,152 +1,138 @@
-// Products with 4-bit weights: RMSNorm -> linear / GLU and the row-scaled linear layer, deferred as in
-// the bf16 kernels, with the codes of fn_w4.h.
-#include "fn_device.h"
-#include "fn_epilogue.h"
-#include "fn_launch.h"
-#include "fn_w4.h"
+// Products with 4-bit weights: which kernel and workgroup shape of w4_kernels.h a call takes, and its launches.
+#include "w4_kernels.h"
 
 namespace fn {
 
-// A workgroup owns 16 rows and NCB column blocks; its KS waves take the 128-row code blocks in turn and
-// their partial products meet in LDS in a fixed order.
-template <int NCB, int KS, int GB, int EPI>
-__global__ __launch_bounds__(64 * KS) void w4_rows_kernel(const __bf16* __restrict__ a, int M, int K, int lda,
-                                                          const void* __restrict__ codes,
-                                                          const unsigned* __restrict__ scales, int NP, int KB,
-                                                          int ncols, __bf16* __restrict__ y, int ldy, EpiArgs ep,
-                                                          int tiles) {
-  constexpr bool kSS = epi_needs_ss(EPI);
-  constexpr int NG = 4 / GB;
-  __shared__ f32x4 red[KS][NCB][64];
-  __shared__ float red_ss[KS][16];
-  const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tile = blockIdx.x % tiles, cb0 = tile * NCB, npb = NP / 16;
-  const int m0 = blockIdx.x / tiles * 16, rows = min(16, M - m0);
-  const int lrow = lane & 15, lch = lane >> 4;
-  const __amdgpu_buffer_rsrc_t rs_a =
-      make_rsrc(a + (int64_t)m0 * lda, (uint32_t)(((int64_t)(rows - 1) * lda + K) * 2));
-  // Column blocks past the packed width (last workgroup only) read other codes, or zeros past the end;
-  // their outputs are never stored.
-  const __amdgpu_buffer_rsrc_t rs_w = make_rsrc(codes, (uint32_t)((int64_t)KB * npb * 1024));
-  const __amdgpu_buffer_rsrc_t rs_s = make_rsrc(scales, (uint32_t)((int64_t)KB * NG * NP * 4));
-  const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u});
+extern template hipError_t launch_w4_few<EPI_RMS>(const W4Args&, int);
+extern template hipError_t launch_w4_few<EPI_GLU>(const W4Args&, int);
+extern template hipError_t launch_w4_few<EPI_ROWSCALE>(const W4Args&, int);
+extern template hipError_t launch_w4_many<EPI_RMS>(const W4Gemm&, int, int, hipStream_t);
+extern template hipError_t launch_w4_many<EPI_GLU>(const W4Gemm&, int, int, hipStream_t);
+extern template hipError_t launch_w4_many<EPI_ROWSCALE>(const W4Gemm&, int, int, hipStream_t);
 
-  f32x4 acc[NCB];
-#pragma unroll
-  for (int c = 0; c < NCB; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float ss = 0.f;
-  for (int kb = wave; kb < KB; kb += KS) {
-    u32x4 wf[NCB], sf[NG][NCB], af[4];
-#pragma unroll
-    for (int c = 0; c < NCB; ++c)
-      wf[c] = load_buf16<kCachePolicyNT>(rs_w, (unsigned)(kb * npb + cb0 + c) * 1024u + lane * 16);
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int k = kb * kW4KB + 32 * u + 8 * lch;
-      af[u] = load_buf16(rs_a, lrow < rows && k < K ? (unsigned)(lrow * lda + k) * 2 : kOobOffset);
+// Workgroup shapes: rows, packed columns, k groups, workgroups that a compute unit holds, and the time in us
+// on MI355X of w workgroups whose waves walk `sets` sets, r = w / 256 the workgroups per compute unit:
+//   start ceil(r / per_cu) + sets (full (ceil(r / per_cu) - 1) + last) + each r,
+// `last` going from one to full as the last round fills up.  Beside it stand what the kernel's launches cost
+// (kW4FewUs, kW4ManyUs), the activations' pass and, with splits of K, the join of their sums.  The constants
+// are least-squares fits over 500 (few rows: 1..200 rows) and 400 (17..2048 rows) random shapes of K 256..11008
+// and 256..22016 columns, linear and GLU, groups of 128, each shape's weights read in turn from 400 MB: 7%
+// rms for the many-row shapes and 10 to 17% for the few-row ones, whose times are launches in large part.  The
+// shape so chosen took 0.7% (many rows) and 3% (few) more than the best of each call.
+struct W4Shape {
+  int rows, cols, ks, per_cu;
+  float start, full, one, each;
+};
+static constexpr W4Shape kW4Few[] = {
+    {16, 32, 8, 2, 0.497f, 1.648f, 0.629f, 0.0f},   {16, 64, 8, 2, 0.510f, 2.514f, 1.137f, 0.0f},
+    {16, 96, 8, 2, 0.0f, 3.959f, 1.652f, 0.815f},   {16, 128, 8, 1, 0.0f, 3.032f, 2.159f, 0.827f},
+    {16, 64, 4, 4, 0.269f, 2.534f, 0.905f, 0.107f}, {16, 32, 4, 4, 0.351f, 1.710f, 0.593f, 0.0f},
+    {16, 16, 8, 2, 0.333f, 1.206f, 0.552f, 0.0f},   {16, 16, 16, 1, 0.113f, 1.506f, 1.072f, 0.0f},
+    {16, 48, 8, 2, 0.619f, 1.946f, 0.886f, 0.007f}};
+static constexpr W4Shape kW4Many[] = {
+    {128, 256, 1, 2, 2.783f, 2.873f, 1.827f, 1.490f}, {128, 128, 1, 2, 1.119f, 1.671f, 1.054f, 1.610f},
+    {96, 256, 1, 2, 1.981f, 2.361f, 1.526f, 1.524f},  {96, 128, 1, 3, 0.646f, 1.884f, 0.868f, 1.465f},
+    {64, 128, 2, 2, 0.339f, 2.016f, 1.175f, 1.665f},  {64, 128, 1, 4, 0.010f, 1.909f, 0.710f, 1.254f},
+    {32, 128, 2, 4, 0.0f, 3.001f, 0.873f, 1.052f},    {32, 64, 4, 2, 0.0f, 1.835f, 0.998f, 0.877f}};
+constexpr int kW4FewLinearOnly = 6;  // from here on: single column blocks hold no gate/up pairs
+constexpr float kW4FewUs = 4.43f, kW4FewPerMK = 1.59f;
+constexpr float kW4ManyUs = 7.69f, kW4ManyPerMK = 0.945f, kW4JoinUs = 2.43f, kW4JoinPerMB = 0.287f;
+// The few-row kernel reads its rows once per column tile and is not looked at beyond this many.
+constexpr int kW4FewMaxM = 256;
+
+static float shape_us(const W4Shape& s, int64_t wgs, int sets) {
+  const float r = (float)wgs / 256.0f, rounds = ceilf(r / s.per_cu);
+  const float in_last = ceilf(r - (rounds - 1.0f) * s.per_cu);
+  const float fill = s.per_cu > 1 ? (in_last - 1.0f) / (s.per_cu - 1) : 0.0f;
+  return s.start * rounds + sets * (s.full * (rounds - 1.0f) + s.one + (s.full - s.one) * fill) + s.each * r;
+}
+
+struct W4Plan {
+  bool many;
+  int shape, splits, kb_per_split;
+};
+
+static W4Plan w4_plan(int M, int K, int KB, int NP, bool glu) {
+  W4Plan best{false, 0, 1, KB};
+  float best_us = 1e30f;
+  const float mk = (float)M * (float)K * 1e-6f;
+  if (M <= kW4FewMaxM) {
+    for (int i = 0; i < (glu ? kW4FewLinearOnly : (int)(sizeof(kW4Few) / sizeof(W4Shape))); ++i) {
+      const W4Shape& s = kW4Few[i];
+      const int64_t wgs = (int64_t)((M + 15) / 16) * ((NP + s.cols - 1) / s.cols);
+      const float us = kW4FewUs + kW4FewPerMK * mk + shape_us(s, wgs, (KB + s.ks - 1) / s.ks);
+      if (us < best_us) best_us = us, best = W4Plan{false, i, 1, KB};
     }
-#pragma unroll
-    for (int j = 0; j < NG; ++j)
-#pragma unroll
-      for (int c = 0; c < NCB; ++c)
-        sf[j][c] = load_buf16(rs_s, (unsigned)((kb * NG + j) * NP + (cb0 + c) * 16 + lch * 4) * 4u);
-#pragma unroll
-    for (int j = 0; j < NG; ++j) {
-      f32x4 part[NCB], sum = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int c = 0; c < NCB; ++c) part[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int u = j * GB; u < (j + 1) * GB; ++u) {
-        bf16x8 av = __builtin_bit_cast(bf16x8, af[u]);
-        if constexpr (kSS) ss = sumsq8(av, ss);
-        bf16x8 lo = __builtin_bit_cast(bf16x8, u32x4{0, 0, 0, 0});
-        if (ep.g_rt) {  // a g as two bf16: its rounding and what that leaves
-          const int k = kb * kW4KB + 32 * u + 8 * lch;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float o = k < K ? (float)av[e] * ep.g_rt[k + e] : 0.0f;
-            av[e] = (__bf16)o;
-            lo[e] = (__bf16)(o - (float)av[e]);
-          }
-          sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, lo, sum, 0, 0, 0);
-#pragma unroll
-          for (int c = 0; c < NCB; ++c)
-            part[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w4_widen(wf[c][u]), lo, part[c], 0, 0, 0);
-        }
-        sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(ones, av, sum, 0, 0, 0);
-#pragma unroll
-        for (int c = 0; c < NCB; ++c)
-          part[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w4_widen(wf[c][u]), av, part[c], 0, 0, 0);
-      }
-#pragma unroll
-      for (int c = 0; c < NCB; ++c)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const unsigned sw = sf[j][c][r];
-          acc[c][r] = fmaf(w4_scale(sw), fmaf(-((float)kW4Bias + w4_zero(sw)), sum[0], part[c][r]), acc[c][r]);
-        }
+    if (M <= 16) return best;
+  }
+  for (int i = 0; i < (int)(sizeof(kW4Many) / sizeof(W4Shape)); ++i) {
+    const W4Shape& s = kW4Many[i];
+    const int64_t tiles = (int64_t)((M + s.rows - 1) / s.rows) * ((NP + s.cols - 1) / s.cols);
+    for (int splits = 1; splits <= 16; splits *= 2) {
+      if (splits > 1 && (tiles * splits > 1100 || KB < 2 * splits)) break;
+      const int per = ((KB + splits - 1) / splits + s.ks - 1) / s.ks * s.ks, n = (KB + per - 1) / per;
+      float us = kW4ManyUs + kW4ManyPerMK * mk + shape_us(s, tiles * n, per / s.ks);
+      if (n > 1) us += kW4JoinUs + kW4JoinPerMB * (float)n * (float)M * (float)NP * 4e-6f;
+      if (us < best_us) best_us = us, best = W4Plan{true, i, n, per};
     }
   }
-  if constexpr (kSS) {
-    ss += __shfl_xor(ss, 16);
-    ss += __shfl_xor(ss, 32);
-  }
-#pragma unroll
-  for (int c = 0; c < NCB; ++c) red[wave][c][lane] = acc[c];
-  if (lane < 16) red_ss[wave][lane] = ss;
-  __syncthreads();
-  const int m = m0 + lrow;
-  if (m >= M) return;
-  float ss_t = 0.f;
-#pragma unroll
-  for (int w = 0; w < KS; ++w) ss_t += red_ss[w][lrow];
-  RowStat st = row_stat<EPI>(ss_t, 0.f, ep);
-  if constexpr (EPI == EPI_ROWSCALE) st.s = ep.row_scale ? ep.row_scale[m] : 1.0f;
-  if constexpr (epi_exports_s(EPI)) {
-    if (ep.inv_rms && tile == 0 && wave == 0 && lane < 16) ep.inv_rms[m] = st.s;
-  }
-  auto total = [&](int c) __attribute__((always_inline)) {
-    f32x4 v = red[0][c][lane];
-#pragma unroll
-    for (int w = 1; w < KS; ++w) v += red[w][c][lane];
-    return v;
+  return best;
+}
+
+// Workspace of a call: the rows' factors, the fp16 activations and the splits' sums; 0 for the few-row kernel.
+static int64_t factor_bytes(int64_t M) { return round_up(M * 4, 256); }
+static int64_t w4_ws(const W4Plan& plan, int64_t M, int64_t KB, int64_t NP) {
+  if (!plan.many) return 0;
+  return factor_bytes(M) + M * KB * (2 * kW4KB) + (plan.splits > 1 ? plan.splits * M * NP * 4 : 0);
+}
+
+int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu) {
+  const int KB = (int)w4_blocks(K);
+  return M > 0 ? w4_ws(w4_plan((int)M, (int)K, KB, (int)NP, glu), M, KB, NP) : 0;
+}
+
+template <bool NORM>
+static hipError_t launch_w4_rows(const W4Args& p, _Float16* out, float* factor) {
+  const int KP = p.KB * kW4KB;
+  auto go = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(p.M), dim3(threads), 0, p.stream, p.a, p.K, p.lda, p.ep.g_rt, p.ep.row_scale, p.ep.eps,
+                       p.ep.inv_k, KP, out, factor, p.ep.inv_rms);
+    return hipGetLastError();
   };
-  constexpr int STEP = epi_is_glu(EPI) ? 2 : 1;
-  for (int o = wave; o < NCB / STEP; o += KS) {
-    const f32x4 v = total(o * STEP), u = STEP == 2 ? total(o * STEP + 1) : v;
-    const int n = (cb0 / STEP + o) * 16 + lch * 4;
-    if (epi_vec<EPI>(ep)) {
-      if (n + 4 <= ncols) store4_bf16_full<EPI, true>(y, ldy, m, n, v, u, st, ep);
-      else store4_bf16_edge<EPI, true>(y, ldy, M, ncols, m, n, v, u, st, ep);
-    } else {
-      if (n + 4 <= ncols) store4_bf16_full<EPI, false>(y, ldy, m, n, v, u, st, ep);
-      else store4_bf16_edge<EPI, false>(y, ldy, M, ncols, m, n, v, u, st, ep);
-    }
-  }
-}
-
-template <int GB, int EPI>
-static hipError_t launch_w4_t(const W4Args& p) {
-  constexpr int NCB = 2, KS = 4;
-  const int tiles = (p.NP / 16 + NCB - 1) / NCB;
-  const int64_t blocks = (int64_t)tiles * ((p.M + 15) / 16);
-  if (blocks * 64 * KS >= (int64_t(1) << 32)) return hipErrorInvalidConfiguration;
-  hipLaunchKernelGGL((w4_rows_kernel<NCB, KS, GB, EPI>), dim3((unsigned)blocks), dim3(64 * KS), 0, p.stream, p.a, p.M, p.K, p.lda, p.codes,
-                     p.scales, p.NP, p.KB, p.ncols, p.y, p.ldy, p.ep, tiles);
-  return hipGetLastError();
-}
-
-template <int EPI>
-static hipError_t launch_w4_epi(const W4Args& p) {
-  return p.group == 32 ? launch_w4_t<1, EPI>(p) : p.group == 64 ? launch_w4_t<2, EPI>(p) : launch_w4_t<4, EPI>(p);
+  // More threads for long rows where rows alone do not fill the chip (64 x 11008: the call 25.1 -> 22.5 us).
+  if (KP <= 8192) return go(w4_rows_kernel<NORM, 256, 4>, 256);
+  if (KP <= 32768) return go(w4_rows_kernel<NORM, 1024, 4>, 1024);
+  return go(w4_rows_kernel<NORM, 1024, 0>, 1024);
 }
 
 hipError_t launch_w4(const W4Args& p) {
+  const bool glu = epi_is_glu(p.epi);
+  const W4Plan plan = w4_plan(p.M, p.K, p.KB, p.NP, glu);
+  const W4Shape& s = plan.many ? kW4Many[plan.shape] : kW4Few[plan.shape];
+  const int64_t groups = (p.M + s.rows - 1) / s.rows, wgs = groups * ((p.NP + s.cols - 1) / s.cols) * plan.splits;
+  // A launch has fewer than 2^32 threads; the pass over the rows has up to 1024 of them each.
+  if (wgs * 512 >= (int64_t(1) << 32) || (plan.many && (int64_t)p.M * 1024 >= (int64_t(1) << 32)))
+    return hipErrorInvalidConfiguration;
+  if (!plan.many) {
+    switch (p.epi) {
+      case EPI_RMS: return launch_w4_few<EPI_RMS>(p, plan.shape);
+      case EPI_GLU: return launch_w4_few<EPI_GLU>(p, plan.shape);
+      case EPI_ROWSCALE: return launch_w4_few<EPI_ROWSCALE>(p, plan.shape);
+    }
+    return hipErrorInvalidValue;
+  }
+  char* ws = static_cast<char*>(p.ws);
+  float* factor = reinterpret_cast<float*>(ws);
+  _Float16* act = reinterpret_cast<_Float16*>(ws + factor_bytes(p.M));
+  float* partial = reinterpret_cast<float*>(ws + factor_bytes(p.M) + (int64_t)p.M * p.KB * (2 * kW4KB));
+  const hipError_t e = p.epi == EPI_ROWSCALE ? launch_w4_rows<false>(p, act, factor) : launch_w4_rows<true>(p, act, factor);
+  if (e != hipSuccess) return e;
+  const W4Gemm q{act, p.M, p.KB * kW4KB, p.codes, p.scales, p.norms, p.NP, p.KB, p.ncols, factor, p.ep.bias, p.y, p.ldy,
+                 (int)groups, plan.splits, plan.kb_per_split, partial};
   switch (p.epi) {
-    case EPI_RMS: return launch_w4_epi<EPI_RMS>(p);
-    case EPI_GLU: return launch_w4_epi<EPI_GLU>(p);
-    case EPI_ROWSCALE: return launch_w4_epi<EPI_ROWSCALE>(p);
+    case EPI_RMS: return launch_w4_many<EPI_RMS>(q, p.group, plan.shape, p.stream);
+    case EPI_GLU: return launch_w4_many<EPI_GLU>(q, p.group, plan.shape, p.stream);
+    case EPI_ROWSCALE: return launch_w4_many<EPI_ROWSCALE>(q, p.group, plan.shape, p.stream);
   }
   return hipErrorInvalidValue;
 }

@@ -76,9 +76,10 @@ def _load():
         "fold_weights_w4": ([P, I64, I64, I, P, I64, I64, I, I, I, P, P], I),
         "pack_weights_w4": ([P, I64, P, I64, P, I64, I64, I64, I, I, P, P], I),
         "unpack_weights_w4": ([P, I64, I64, I, I, P, I64, P], I),
-        "flashnorm_linear_w4": ([P, I64, I64, I64, I, P, P, I64, I, F, P, P, I64, I, P, P], I),
-        "flashnorm_glu_w4": ([P, I64, I64, I64, I, P, P, I64, I, F, P, I64, I, P], I),
-        "rowscale_linear_w4": ([P, I64, I64, I64, I, P, I64, I, P, P, I64, I, P], I),
+        "flashnorm_w4_workspace_size": ([I64, I64, I64, I], ctypes.c_size_t),
+        "flashnorm_linear_w4": ([P, I64, I64, I64, I, P, P, I64, I, F, P, P, I64, I, P, P, ctypes.c_size_t, P], I),
+        "flashnorm_glu_w4": ([P, I64, I64, I64, I, P, P, I64, I, F, P, I64, I, P, ctypes.c_size_t, P], I),
+        "rowscale_linear_w4": ([P, I64, I64, I64, I, P, I64, I, P, P, I64, I, P, ctypes.c_size_t, P], I),
         "flashnorm_block_residual": ([P, I64, P, I64, I64, I64, I, P, F, P, I64, I64, F, F, P, F, P, I64, P, I64, P, P],
                                      I),
         "flashnorm_block_residual_bwd_size": ([I64, I64, I64, I], ctypes.c_size_t),
@@ -641,6 +642,23 @@ def unpack_weights_w4(w4: W4Weight, stream=None) -> torch.Tensor:
     return out
 
 
+@functools.lru_cache(maxsize=4096)
+def _w4_workspace(M, K, N, layout):  # a pure function of the four, asked again by every call
+    return _load().flashnorm_w4_workspace_size(M, K, N, layout)
+
+
+def _workspace(where, workspace, need, like):
+    """The caller's workspace, checked, or a new one; None where none is needed."""
+    if not need:
+        return None
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=like.device)
+    if workspace.get_device() != like.get_device() or not workspace.is_contiguous() or \
+            workspace.numel() * workspace.element_size() < need:
+        raise ValueError(f"{where}: the workspace must be {need} contiguous bytes on {like.device}")
+    return workspace
+
+
 def _w4_args(where, a, w4, layout, N, out):
     """Checks of a product's operands; returns M, K, the type code and the output."""
     M, K = a.shape
@@ -656,43 +674,49 @@ def _w4_args(where, a, w4, layout, N, out):
 
 
 def flashnorm_linear_w4(a: torch.Tensor, w4: W4Weight, eps: float, g=None, bias=None, out=None, inv_rms=None,
-                        stream=None) -> torch.Tensor:
+                        workspace=None, stream=None) -> torch.Tensor:
     """y = RMSNorm(a) W4 (+ bias), deferred; g: the norm weight, where it is not folded into w4."""
     if _elsewhere(a, stream):
         with _current("flashnorm_linear_w4", a, stream):
-            return flashnorm_linear_w4(a, w4, eps, g, bias, out, inv_rms)
+            return flashnorm_linear_w4(a, w4, eps, g, bias, out, inv_rms, workspace)
     N = w4.N
     M, K, code, y = _w4_args("flashnorm_linear_w4", a, w4, FN_LAYOUT_LINEAR, N, out)
     _on_gpu("flashnorm_linear_w4", a, w4.data, y, g, bias, inv_rms)
+    need = _w4_workspace(M, K, w4.N, w4.layout)
+    ws = _workspace("flashnorm_linear_w4", workspace, need, a)
     _check(_load().flashnorm_linear_w4(a.data_ptr(), M, K, _ld(a), code, _ptr(_vec(g, K, "g")), w4.data.data_ptr(), N,
                                        w4.group, eps, _ptr(_vec(bias, N, "bias")), y.data_ptr(), _ld(y), code,
-                                       _ptr(_vec(inv_rms, M, "inv_rms")), _stream(None)), "flashnorm_linear_w4")
+                                       _ptr(_vec(inv_rms, M, "inv_rms")), _ptr(ws), need, _stream(None)), "flashnorm_linear_w4")
     return y
 
 
-def flashnorm_glu_w4(a: torch.Tensor, w4: W4Weight, eps: float, g=None, out=None, stream=None) -> torch.Tensor:
+def flashnorm_glu_w4(a: torch.Tensor, w4: W4Weight, eps: float, g=None, out=None, workspace=None, stream=None) -> torch.Tensor:
     """silu(RMSNorm(a) Wg) * (RMSNorm(a) Wu) with w4 = [Wg | Wu] (FN_LAYOUT_GLU)."""
     if _elsewhere(a, stream):
         with _current("flashnorm_glu_w4", a, stream):
-            return flashnorm_glu_w4(a, w4, eps, g, out)
+            return flashnorm_glu_w4(a, w4, eps, g, out, workspace)
     F = w4.N // 2
     M, K, code, o = _w4_args("flashnorm_glu_w4", a, w4, FN_LAYOUT_GLU, F, out)
     _on_gpu("flashnorm_glu_w4", a, w4.data, o, g)
+    need = _w4_workspace(M, K, w4.N, w4.layout)
+    ws = _workspace("flashnorm_glu_w4", workspace, need, a)
     _check(_load().flashnorm_glu_w4(a.data_ptr(), M, K, _ld(a), code, _ptr(_vec(g, K, "g")), w4.data.data_ptr(), F,
-                                    w4.group, eps, o.data_ptr(), _ld(o), code, _stream(None)), "flashnorm_glu_w4")
+                                    w4.group, eps, o.data_ptr(), _ld(o), code, _ptr(ws), need, _stream(None)), "flashnorm_glu_w4")
     return o
 
 
-def rowscale_linear_w4(x: torch.Tensor, w4: W4Weight, row_scale=None, out=None, stream=None) -> torch.Tensor:
+def rowscale_linear_w4(x: torch.Tensor, w4: W4Weight, row_scale=None, out=None, workspace=None, stream=None) -> torch.Tensor:
     """y = (x W4) * row_scale[m], or x W4: a down projection, with a deferred norm's scale or without."""
     if _elsewhere(x, stream):
         with _current("rowscale_linear_w4", x, stream):
-            return rowscale_linear_w4(x, w4, row_scale, out)
+            return rowscale_linear_w4(x, w4, row_scale, out, workspace)
     N = w4.N
     M, K, code, y = _w4_args("rowscale_linear_w4", x, w4, FN_LAYOUT_LINEAR, N, out)
     _on_gpu("rowscale_linear_w4", x, w4.data, y, row_scale)
+    need = _w4_workspace(M, K, w4.N, w4.layout)
+    ws = _workspace("rowscale_linear_w4", workspace, need, x)
     _check(_load().rowscale_linear_w4(x.data_ptr(), M, K, _ld(x), code, w4.data.data_ptr(), N, w4.group,
-                                      _ptr(_vec(row_scale, M, "row_scale")), y.data_ptr(), _ld(y), code, _stream(None)),
+                                      _ptr(_vec(row_scale, M, "row_scale")), y.data_ptr(), _ld(y), code, _ptr(ws), need, _stream(None)),
            "rowscale_linear_w4")
     return y
 

@@ -15,18 +15,19 @@ def lib():
 
 def test_size(lib):
     f = lib.fold_weights_w4_size
-    # half a byte per weight of the padded shape, four bytes per group and packed column
-    assert f(4096, 11008, 0, 128) == 4096 * 11008 // 2 + 32 * 11008 * 4
-    assert f(4096, 11008, 0, 32) == 4096 * 11008 // 2 + 128 * 11008 * 4
-    assert f(8, 3, 0, 128) == 128 * 16 // 2 + 16 * 4
-    assert f(136, 2 * 9, 1, 64) == 256 * 32 // 2 + 4 * 32 * 4
+    # half a byte per weight of the padded shape, four bytes per group and packed column and four per column
+    assert f(4096, 11008, 0, 128) == 4096 * 11008 // 2 + (32 + 1) * 11008 * 4
+    assert f(4096, 11008, 0, 32) == 4096 * 11008 // 2 + (128 + 1) * 11008 * 4
+    assert f(8, 3, 0, 128) == 128 * 16 // 2 + (1 + 1) * 16 * 4
+    assert f(136, 2 * 9, 1, 64) == 256 * 32 // 2 + (4 + 1) * 32 * 4
     for bad in ((0, 16, 0, 32), (16, 0, 0, 32), (16, 7, 1, 32), (16, 16, 2, 32), (16, 16, 0, 48), (16, 16, 0, 0),
                 (1 << 16, 1 << 16, 0, 128), ((1 << 21) + 8, 16, 0, 128)):
         assert f(*bad) == 0, bad
 
 
-def _lin(lib, a=A, M=4, K=64, lda=64, adt=1, g=0, w=W, N=32, group=32, eps=1e-6, bias=0, y=Y, ldy=32, ydt=1, inv=0):
-    return lib.flashnorm_linear_w4(a, M, K, lda, adt, g, w, N, group, eps, bias, y, ldy, ydt, inv, None)
+def _lin(lib, a=A, M=4, K=64, lda=64, adt=1, g=0, w=W, N=32, group=32, eps=1e-6, bias=0, y=Y, ldy=32, ydt=1, inv=0, ws=0,
+         wb=0):
+    return lib.flashnorm_linear_w4(a, M, K, lda, adt, g, w, N, group, eps, bias, y, ldy, ydt, inv, ws, wb, None)
 
 
 def test_products_refuse(lib):
@@ -58,11 +59,20 @@ def test_products_refuse(lib):
     assert _lin(lib, inv=Y) == -8
     assert _lin(lib, inv=A) == -8
     assert _lin(lib, lda=1 << 22) == -9
-    assert _lin(lib, M=1 << 30, K=8, lda=8, N=1 << 20, ldy=1 << 20, y=1 << 60) == -9   # more workgroups than a launch takes
+    big = dict(M=1 << 30, K=8, lda=8, N=1 << 20, ldy=1 << 20, y=1 << 60)
+    assert _lin(lib, ws=1 << 61, wb=1 << 59, **big) == -9   # more workgroups than a launch takes
+    assert _lin(lib, M=1000) == -1                          # a workspace is needed
+    need = lib.flashnorm_w4_workspace_size(1000, 64, 32, 0)
+    assert need > 1000 * 64 * 2
+    assert _lin(lib, M=1000, ws=B, wb=need - 1) == -9
+    assert _lin(lib, M=1000, ws=B + 8, wb=need) == -4
+    assert _lin(lib, M=1000, ws=Y, wb=need) == -8 and _lin(lib, M=1000, ws=A, wb=need) == -8
+    f = lib.flashnorm_w4_workspace_size
+    assert f(16, 4096, 4096, 0) == 0 and f(0, 64, 32, 0) == 0 and f(-1, 64, 32, 0) == 0 and f(1000, 64, 31, 1) == 0
     assert _lin(lib, M=0, a=0, y=0) == 0
-    glu = lambda F=16, ldo=16, w=W: lib.flashnorm_glu_w4(A, 4, 64, 64, 1, None, w, F, 32, 1e-6, Y, ldo, 1, None)
+    glu = lambda F=16, ldo=16, w=W: lib.flashnorm_glu_w4(A, 4, 64, 64, 1, None, w, F, 32, 1e-6, Y, ldo, 1, None, 0, None)
     assert glu(F=0) == -2 and glu(ldo=8) == -2 and glu(w=0) == -1
-    row = lambda rs=0, y=Y: lib.rowscale_linear_w4(A, 4, 64, 64, 1, W, 32, 32, rs, y, 32, 1, None)
+    row = lambda rs=0, y=Y: lib.rowscale_linear_w4(A, 4, 64, 64, 1, W, 32, 32, rs, y, 32, 1, None, 0, None)
     assert row(y=A) == -8 and row(rs=Y) == -8 and row(rs=X + 2) == -4
 
 
