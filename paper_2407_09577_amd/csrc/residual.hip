@@ -45,27 +45,43 @@ __device__ __forceinline__ void load_f32(const float* p, float (&v)[N]) {
   }
 }
 
-// Sums of NV values over the TPR threads of a row, the same in all of them and in a fixed order.  One wave
-// exchanges within itself; more meet in LDS, in the two halves of buf by turns, so one barrier a call
-// is enough: a wave writes a half again only after the barrier of the call between.
+// The sum over the first N = 2, 4, 8 or 16 lanes of each sixteen, where they repeat with that period, in every
+// lane and in a fixed order.
+template <int N>
+__device__ __forceinline__ float lanes_total(float v) {
+  auto add = [&](auto ctrl) __attribute__((always_inline)) {
+    v += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), decltype(ctrl)::value, 0xf, 0xf, true));
+  };
+  add(std::integral_constant<int, 0xb1>{});                           // lanes 1, 0, 3, 2
+  if constexpr (N >= 4) add(std::integral_constant<int, 0x4e>{});     // lanes 2, 3, 0, 1
+  if constexpr (N >= 8) add(std::integral_constant<int, 0x141>{});    // 7 - i of eight
+  if constexpr (N >= 16) add(std::integral_constant<int, 0x140>{});   // 15 - i of sixteen
+  return v;
+}
+
+__device__ __forceinline__ float wave_total(float v) {
+  v = lanes_total<16>(v);
+  auto row = [&](int l) __attribute__((always_inline)) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l));
+  };
+  return (row(0) + row(16)) + (row(32) + row(48));
+}
+
+// Sums of NV values over the TPR threads of a row, the same in all of them and in a fixed order.  Several
+// waves meet in LDS, in the two halves of buf by turns, so one barrier a call is enough: a wave writes a half
+// again only after the barrier of the call between.
 template <int TPR, int NV>
-__device__ __forceinline__ void row_sum(float (&v)[NV], float (*buf)[TPR / 64][NV], int& turn) {
+__device__ __forceinline__ void row_sum(float (&v)[NV], float (*buf)[NV][TPR / 64], int& turn) {
 #pragma unroll
-  for (int o = 32; o >= 1; o >>= 1)
-#pragma unroll
-    for (int i = 0; i < NV; ++i) v[i] += __shfl_xor(v[i], o);
+  for (int i = 0; i < NV; ++i) v[i] = wave_total(v[i]);
   if constexpr (TPR > 64) {
     if ((threadIdx.x & 63) == 0) {
 #pragma unroll
-      for (int i = 0; i < NV; ++i) buf[turn][threadIdx.x >> 6][i] = v[i];
+      for (int i = 0; i < NV; ++i) buf[turn][i][threadIdx.x >> 6] = v[i];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      v[i] = buf[turn][0][i];
-#pragma unroll
-      for (int w = 1; w < TPR / 64; ++w) v[i] += buf[turn][w][i];
-    }
+    for (int i = 0; i < NV; ++i) v[i] = lanes_total<TPR / 64>(buf[turn][i][threadIdx.x & (TPR / 64 - 1)]);
     turn ^= 1;
   }
 }
@@ -74,7 +90,7 @@ __device__ __forceinline__ void row_sum(float (&v)[NV], float (*buf)[TPR / 64][N
 template <typename T, int TPR, int V>
 __global__ __launch_bounds__(TPR) void residual_kernel(ResidualArgs p) {
   constexpr int VN = Vec<T>::N;
-  __shared__ float buf[2][TPR / 64][1];
+  __shared__ float buf[2][1][TPR / 64];
   int turn = 0;
   const int K = p.K;
   const float inv_k = 1.0f / (float)K;
@@ -148,19 +164,20 @@ __global__ __launch_bounds__(TPR) void residual_kernel(ResidualArgs p) {
   }
 }
 
-// How the backward pass cuts the rows into units, each one workgroup's: ranges of rows that hold whole
-// gate segments (seg_per_unit > 0, dgate written by the unit) or lie in one (pieces per segment, dgate
-// from partial sums).  Without a gate, or with one per row, the rows are cut evenly.
+// How the backward pass cuts the rows into units, each one workgroup's: ranges of rows that hold whole gate
+// segments (pieces = 0: dgate is the unit's to write) or lie in one (pieces units per segment: dgate comes
+// from their partial sums).  Without a gate, or with one per row, the rows are cut evenly.
 struct Units {
   int64_t count;
-  int rows;          // rows of a unit
-  int pieces;        // units per segment; 0: units hold whole segments or there is no sum over rows
+  int rows, pieces;
 };
 
-Units units_of(int64_t M, int64_t gate_rows, bool gate) {
-  const int64_t kUnits = 1024;
+// Enough units to fill the chip (eight waves per SIMD for narrow rows, four for wide), and no more: each
+// leaves a row of fp32 partial sums per parameter.
+Units units_of(int64_t M, int64_t gate_rows, bool gate, int tpr) {
+  const int64_t most = tpr <= 128 ? 2048 : tpr == 256 ? 1024 : 512;
   if (M == 0) return Units{0, 0, 0};
-  int64_t rows = (M + kUnits - 1) / kUnits;
+  int64_t rows = (M + most - 1) / most;
   if (!gate || gate_rows == 1) return Units{(M + rows - 1) / rows, (int)rows, 0};
   const int64_t segs = (M + gate_rows - 1) / gate_rows, T = gate_rows < M ? gate_rows : M;
   if (T <= rows) {
@@ -177,97 +194,152 @@ Units units_of(int64_t M, int64_t gate_rows, bool gate) {
 //   D  = dH + r (a - H r t),  t = r sum(a H) / K           the gradient at H
 //   dh = res_scale D,  dx = p (branch_scale gate g_post D - x p q),  q = p sum(v D) / K
 // and sum(v D) = sum(v dH) + r (sum(v a) - r t sum(v H)), so the five sums that D and dx need are taken
-// in one pass over the row in registers, after the first one (p).
-template <typename T, int TPR, int V>
-__global__ __launch_bounds__(TPR) void residual_bwd_kernel(ResidualArgs p, Units un, float* part_post, float* part_pre,
+// in one pass over the row, after the first one (p).  The parameters' gradients add up in registers over the
+// unit's rows.  Two workgroups of eight waves a compute unit hide each other's waits: with the next row's
+// loads held ahead in registers only one fits (4096 x 4096 bf16, gate and both norms: 56 us, 45 without).
+template <typename T, int TPR, int V, bool POST, bool PRE>
+__global__ __launch_bounds__(TPR, TPR >= 512 ? 4 : 1) void residual_bwd_kernel(ResidualArgs p, Units un, float* part_post, float* part_pre,
                                                            float* part_gate) {
   constexpr int VN = Vec<T>::N;
-  __shared__ float buf1[2][TPR / 64][1];
-  __shared__ float buf5[2][TPR / 64][5];
+  __shared__ float buf1[2][1][TPR / 64];
+  __shared__ float buf5[2][5][TPR / 64];
   int turn1 = 0, turn5 = 0;
   const int K = p.K;
   const float inv_k = 1.0f / (float)K;
   const int64_t u = blockIdx.x;
   int64_t m0, m1;
   if (un.pieces) {
-    const int64_t seg = u / un.pieces, s0 = seg * p.gate_rows;
-    m0 = s0 + (u % un.pieces) * un.rows;
+    const int64_t s0 = u / un.pieces * p.gate_rows;
+    m0 = s0 + u % un.pieces * un.rows;
     m1 = min(min(m0 + un.rows, s0 + (int64_t)p.gate_rows), (int64_t)p.M);
   } else {
     m0 = u * un.rows;
     m1 = min(m0 + un.rows, (int64_t)p.M);
   }
-  float gpost[V][VN], gpre[V][VN], apost[V][VN], apre[V][VN], agate[V][VN];
+  // The sums over the unit's rows: in registers, but those of the norms' weights in LDS where a thread has
+  // sixteen columns and no registers for them (each thread its own columns, so no barrier).
+  constexpr bool kLds = V * VN >= 16;
+  constexpr int VR = kLds ? 1 : V;
+  __shared__ float lpost[kLds && POST ? V * VN : 1][kLds && POST ? TPR : 1];
+  __shared__ float lpre[kLds && PRE ? V * VN : 1][kLds && PRE ? TPR : 1];
+  float apost[VR][VN], apre[VR][VN], agate[V][VN];
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
+  for (int j = 0; j < V; ++j)
+#pragma unroll
+    for (int e = 0; e < VN; ++e) {
+      agate[j][e] = 0.0f;
+      if constexpr (!kLds) apost[j][e] = apre[j][e] = 0.0f;
+      if constexpr (kLds && POST) lpost[j * VN + e][threadIdx.x] = 0.0f;
+      if constexpr (kLds && PRE) lpre[j * VN + e][threadIdx.x] = 0.0f;
+    }
+  // A thread's piece j of a row.  Lanes past K, and what a call has not, hold zeros (the gate: ones).
+  struct Piece {
+    Vec<T> x, h, gate, dho, dn;
+    float gpost[VN], gpre[VN];
+  };
+  auto load_g = [&](int j, Piece& c) __attribute__((always_inline)) {
     const int k = (j * TPR + threadIdx.x) * VN;
 #pragma unroll
-    for (int e = 0; e < VN; ++e) gpost[j][e] = 1.0f, gpre[j][e] = apost[j][e] = apre[j][e] = agate[j][e] = 0.0f;
-    if (k < K && p.g_post) load_f32(p.g_post + k, gpost[j]);
-    if (k < K && p.g_pre) load_f32(p.g_pre + k, gpre[j]);
-  }
-  for (int64_t m = m0; m < m1; ++m) {
-    Vec<T> x[V], h[V], gate[V], dho[V], dn[V];
-    float ss[1] = {0.f};
+    for (int e = 0; e < VN; ++e) c.gpost[e] = c.gpre[e] = 0.0f;
+    if (k < K && POST) load_f32(p.g_post + k, c.gpost);
+    if (k < K && PRE) load_f32(p.g_pre + k, c.gpre);
+  };
+  const u32x4 one = sizeof(T) == 2 ? u32x4{0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}
+                                   : u32x4{0x3f800000u, 0x3f800000u, 0x3f800000u, 0x3f800000u};
+  auto load = [&](int64_t m, int j, Piece& c) __attribute__((always_inline)) {
+    const int k = (j * TPR + threadIdx.x) * VN;
+    c.x.w = c.h.w = c.dho.w = c.dn.w = u32x4{0, 0, 0, 0};
+    c.gate.w = one;
+    if (k >= K) return;
+    c.x.load((const T*)p.x + m * p.ldx + k);
+    c.h.load((const T*)p.h + m * p.ldh + k);
+    if (p.gate) c.gate.load((const T*)p.gate + m / p.gate_rows * p.ldg + k);
+    if (p.dh_out) c.dho.load((const T*)p.dh_out + m * p.lddo + k);
+    if constexpr (PRE) c.dn.load((const T*)p.dn + m * p.lddn + k);
+  };
+  // One piece a thread stays in registers over the row's three passes; with more each pass reads them again
+  // (from the caches), as the three sums of every column leave no room to hold them.
+  Piece c;
+  if constexpr (V == 1) load_g(0, c);
+  auto pass = [&](int64_t m, auto body) __attribute__((always_inline)) {
+    if constexpr (V == 1) {
+      body(0);
+    } else {
+      asm volatile("" ::: "memory");  // or the passes' equal loads become one, held in spilled registers
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int k = (j * TPR + threadIdx.x) * VN;
-      x[j].w = h[j].w = gate[j].w = dho[j].w = dn[j].w = u32x4{0, 0, 0, 0};
-      if (k < K) {
-        x[j].load((const T*)p.x + m * p.ldx + k);
-        h[j].load((const T*)p.h + m * p.ldh + k);
-        if (p.gate) gate[j].load((const T*)p.gate + m / p.gate_rows * p.ldg + k);
-        if (p.dh_out) dho[j].load((const T*)p.dh_out + m * p.lddo + k);
-        if (p.dn) dn[j].load((const T*)p.dn + m * p.lddn + k);
+      for (int j = 0; j < V; ++j) {
+        load_g(j, c);
+        load(m, j, c);
+        body(j);
+        __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-      for (int e = 0; e < VN; ++e) ss[0] = fmaf(x[j][e], x[j][e], ss[0]);
     }
+  };
+  for (int64_t m = m0; m < m1; ++m) {
+    if constexpr (V == 1) load(m, 0, c);
     float rp = 1.0f;
-    if (p.g_post) {
+    if constexpr (POST) {
+      float ss[1] = {0.f};
+      pass(m, [&](int) __attribute__((always_inline)) {
+#pragma unroll
+        for (int e = 0; e < VN; ++e) ss[0] = fmaf(c.x[e], c.x[e], ss[0]);
+      });
       row_sum<TPR, 1>(ss, buf1, turn1);
       rp = rsqrtf(fmaf(ss[0], inv_k, p.eps_post));
     }
-    float s5[5] = {0.f, 0.f, 0.f, 0.f, 0.f};  // H^2, a H, v dH, v a, v H
-    auto scale_at = [&](int j, int e) { return p.gate ? p.branch_scale * gate[j][e] : p.branch_scale; };
-    auto H_at = [&](int j, int e) {
-      return fmaf(scale_at(j, e) * gpost[j][e] * rp, x[j][e], p.res_scale * h[j][e]);
+    float r = 0.f, t = 0.f, q = 0.f;
+    auto scale = [&](int e) __attribute__((always_inline)) { return p.branch_scale * c.gate[e]; };
+    auto branch = [&](int e) __attribute__((always_inline)) {  // v
+      return (POST ? scale(e) * c.gpost[e] : scale(e)) * c.x[e];
     };
+    auto H_of = [&](int e, float v) __attribute__((always_inline)) { return fmaf(v, rp, p.res_scale * c.h[e]); };
+    if constexpr (POST || PRE) {
+      float s5[5] = {0.f, 0.f, 0.f, 0.f, 0.f};  // H^2, a H, v dH, v a, v H
+      pass(m, [&](int) __attribute__((always_inline)) {
 #pragma unroll
-    for (int j = 0; j < V; ++j)
-#pragma unroll
-      for (int e = 0; e < VN; ++e) {
-        const float H = H_at(j, e), a = dn[j][e] * gpre[j][e], v = scale_at(j, e) * gpost[j][e] * x[j][e];
-        s5[0] = fmaf(H, H, s5[0]);
-        s5[1] = fmaf(a, H, s5[1]);
-        s5[2] = fmaf(v, dho[j][e], s5[2]);
-        s5[3] = fmaf(v, a, s5[3]);
-        s5[4] = fmaf(v, H, s5[4]);
+        for (int e = 0; e < VN; ++e) {
+          const float v = branch(e);
+          if constexpr (PRE) {
+            const float H = H_of(e, v), a = c.dn[e] * c.gpre[e];
+            s5[0] = fmaf(H, H, s5[0]);
+            s5[1] = fmaf(a, H, s5[1]);
+            s5[3] = fmaf(v, a, s5[3]);
+            s5[4] = fmaf(v, H, s5[4]);
+          }
+          s5[2] = fmaf(v, c.dho[e], s5[2]);
+        }
+      });
+      row_sum<TPR, 5>(s5, buf5, turn5);
+      if constexpr (PRE) {
+        r = rsqrtf(fmaf(s5[0], inv_k, p.eps_pre));
+        t = r * s5[1] * inv_k;
       }
-    row_sum<TPR, 5>(s5, buf5, turn5);
-    const float r = p.g_pre ? rsqrtf(fmaf(s5[0], inv_k, p.eps_pre)) : 0.0f;
-    const float t = r * s5[1] * inv_k;
-    const float q = rp * (s5[2] + r * (s5[3] - r * t * s5[4])) * inv_k;
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-      const int k = (j * TPR + threadIdx.x) * VN;
-      if (k >= K) continue;
-      float odx[VN], odh[VN], og[VN];
-#pragma unroll
-      for (int e = 0; e < VN; ++e) {
-        const float H = H_at(j, e), a = dn[j][e] * gpre[j][e], sc = scale_at(j, e);
-        const float D = p.g_pre ? fmaf(r, fmaf(-(H * r), t, a), dho[j][e]) : dho[j][e];
-        const float xp = x[j][e] * rp, dz = sc * D;
-        odh[e] = p.res_scale * D;
-        odx[e] = p.g_post ? rp * fmaf(-xp, q, dz * gpost[j][e]) : dz;
-        og[e] = p.branch_scale * D * xp * gpost[j][e];
-        apost[j][e] = fmaf(dz, xp, apost[j][e]);
-        apre[j][e] = fmaf(dn[j][e], H * r, apre[j][e]);
-        agate[j][e] += og[e];
-      }
-      store_vec<T>((T*)p.dx + m * p.lddx + k, odx);
-      store_vec<T>((T*)p.dh + m * p.lddh + k, odh);
+      q = rp * (s5[2] + r * (s5[3] - r * t * s5[4])) * inv_k;
     }
+    pass(m, [&](int j) __attribute__((always_inline)) {
+      const int k = (j * TPR + threadIdx.x) * VN;
+      float odx[VN], odh[VN];
+#pragma unroll
+      for (int e = 0; e < VN; ++e) {
+        float D = c.dho[e];
+        if constexpr (PRE) {
+          const float Hr = H_of(e, branch(e)) * r;
+          D = fmaf(r, fmaf(-Hr, t, c.dn[e] * c.gpre[e]), D);
+          if constexpr (kLds) lpre[j * VN + e][threadIdx.x] = fmaf(c.dn[e], Hr, lpre[j * VN + e][threadIdx.x]);
+          else apre[j][e] = fmaf(c.dn[e], Hr, apre[j][e]);
+        }
+        const float xp = c.x[e] * rp, dz = scale(e) * D, Dx = D * xp;
+        odh[e] = p.res_scale * D;
+        odx[e] = POST ? rp * fmaf(-xp, q, dz * c.gpost[e]) : dz;
+        agate[j][e] = fmaf(POST ? Dx * c.gpost[e] : Dx, p.branch_scale, agate[j][e]);
+        if constexpr (POST && kLds) lpost[j * VN + e][threadIdx.x] = fmaf(dz, xp, lpost[j * VN + e][threadIdx.x]);
+        else if constexpr (POST) apost[j][e] = fmaf(dz, xp, apost[j][e]);
+      }
+      if (k < K) {
+        store_vec<T>((T*)p.dx + m * p.lddx + k, odx);
+        store_vec<T>((T*)p.dh + m * p.lddh + k, odh);
+      }
+    });
     // The gate row's sum, where the unit holds all of its rows.
     if (p.dgate && !un.pieces && (m + 1 == m1 || (m + 1) % p.gate_rows == 0)) {
 #pragma unroll
@@ -279,71 +351,106 @@ __global__ __launch_bounds__(TPR) void residual_bwd_kernel(ResidualArgs p, Units
       }
     }
   }
+  auto keep = [&](float* part, auto value) __attribute__((always_inline)) {
+    if (!part) return;
 #pragma unroll
-  for (int j = 0; j < V; ++j) {
-    const int k = (j * TPR + threadIdx.x) * VN;
-    if (k >= K) continue;
+    for (int j = 0; j < V; ++j) {
+      const int k = (j * TPR + threadIdx.x) * VN;
+      if (k >= K) continue;
 #pragma unroll
-    for (int i = 0; i < VN; i += 4) {
-      const int64_t at = u * K + k + i;
-      if (part_post)
-        *reinterpret_cast<f32x4*>(part_post + at) = f32x4{apost[j][i], apost[j][i + 1], apost[j][i + 2], apost[j][i + 3]};
-      if (part_pre)
-        *reinterpret_cast<f32x4*>(part_pre + at) = f32x4{apre[j][i], apre[j][i + 1], apre[j][i + 2], apre[j][i + 3]};
-      if (part_gate)
-        *reinterpret_cast<f32x4*>(part_gate + at) = f32x4{agate[j][i], agate[j][i + 1], agate[j][i + 2], agate[j][i + 3]};
+      for (int i = 0; i < VN; i += 4)
+        *reinterpret_cast<f32x4*>(part + u * K + k + i) =
+            f32x4{value(j, i), value(j, i + 1), value(j, i + 2), value(j, i + 3)};
+    }
+  };
+  if constexpr (POST)
+    keep(part_post, [&](int j, int e) {
+      if constexpr (kLds) return lpost[j * VN + e][threadIdx.x];
+      else return apost[j][e];
+    });
+  if constexpr (PRE)
+    keep(part_pre, [&](int j, int e) {
+      if constexpr (kLds) return lpre[j * VN + e][threadIdx.x];
+      else return apre[j][e];
+    });
+  keep(part_gate, [&](int j, int e) { return agate[j][e]; });
+}
+
+// Sums of the units' partials in a fixed order.  A workgroup takes 32 columns of one sum (blockIdx.y: dg_post,
+// dg_pre, then the gate's segments, as far as the call has them): eight threads read 128 bytes of a partial
+// row, 32 rows at a time.
+template <typename T>
+__global__ __launch_bounds__(256) void residual_sums_kernel(ResidualArgs p, Units un, const float* part_post,
+                                                            const float* part_pre, const float* part_gate) {
+  __shared__ f32x4 red[32][8];
+  const int q = threadIdx.x & 7, w = threadIdx.x >> 3, k = (blockIdx.x * 8 + q) * 4, K = p.K;
+  int which = blockIdx.y;
+  const float* part = nullptr;
+  float* out = nullptr;
+  int64_t count = un.count;
+  if (p.dg_post && which-- == 0) part = part_post, out = p.dg_post;
+  else if (p.dg_pre && which-- == 0) part = part_pre, out = p.dg_pre;
+  else part = part_gate + (int64_t)which * un.pieces * K, count = un.pieces;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (k < K) {
+    for (int64_t u0 = w; u0 < count; u0 += 32 * 8) {
+      f32x4 v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (u0 + 32 * i < count) v[i] = *reinterpret_cast<const f32x4*>(part + (u0 + 32 * i) * K + k);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += v[i];
     }
   }
-}
-
-// Sums of the units' partials in a fixed order: out[s][k] = sum over the `count` units of segment s.
-template <typename T>
-__global__ __launch_bounds__(1024) void residual_reduce_kernel(const float* __restrict__ part, int K, int64_t count,
-                                                               T* __restrict__ out, int64_t ldo) {
-  __shared__ float red[16][64];
-  const int k = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
-  const int64_t seg = blockIdx.y;
-  float s = 0.f;
-  if (k < K)
-    for (int64_t u = w; u < count; u += 16) s += part[(seg * count + u) * K + k];
-  red[w][threadIdx.x & 63] = s;
+  red[w][q] = s;
   __syncthreads();
-  if (w == 0 && k < K) {
+  if (w || k >= K) return;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) s += red[i][threadIdx.x];
-    if constexpr (sizeof(T) == 2) out[seg * ldo + k] = (T)s;
-    else out[seg * ldo + k] = s;
+  for (int i = 1; i < 32; ++i) s += red[i][q];
+  if (out) {
+    *reinterpret_cast<f32x4*>(out + k) = s;
+  } else if constexpr (sizeof(T) == 2) {
+    const float o[4] = {s[0], s[1], s[2], s[3]};
+    *reinterpret_cast<u32x2*>((T*)p.dgate + (int64_t)which * p.lddg + k) = pack4_bf16(o);
+  } else {
+    *reinterpret_cast<f32x4*>((T*)p.dgate + (int64_t)which * p.lddg + k) = s;
   }
 }
 
-// Threads per row and vectors per thread: K <= threads * vectors * (16 bytes).
+// Threads per row and vectors per thread: the fewest threads that hold the row's n vectors of 16 bytes one
+// apiece; 1024 threads with two or four beyond.
+int threads_of(int64_t K, int dtype) {
+  const int64_t n = K / (dtype == kDtypeBf16 ? 8 : 4);
+  return n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : n <= 512 ? 512 : 1024;
+}
+
 template <typename T, typename F>
 hipError_t with_shape(int K, F go) {
-  const int n = (K + Vec<T>::N - 1) / Vec<T>::N;  // vectors of a row
+  const int n = K / Vec<T>::N;
   if (n <= 64) return go(std::integral_constant<int, 64>{}, std::integral_constant<int, 1>{});
   if (n <= 128) return go(std::integral_constant<int, 128>{}, std::integral_constant<int, 1>{});
   if (n <= 256) return go(std::integral_constant<int, 256>{}, std::integral_constant<int, 1>{});
   if (n <= 512) return go(std::integral_constant<int, 512>{}, std::integral_constant<int, 1>{});
   if (n <= 1024) return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 1>{});
   if (n <= 2048) return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 2>{});
-  return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
+  if constexpr (sizeof(T) == 4) return go(std::integral_constant<int, 1024>{}, std::integral_constant<int, 4>{});
+  return hipErrorInvalidValue;
 }
 
 template <typename T>
 hipError_t launch_fwd_t(const ResidualArgs& p) {
   return with_shape<T>(p.K, [&](auto tpr, auto v) {
     constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value;
-    if constexpr (sizeof(T) == 2 && V > 2) return hipErrorInvalidValue;
-    else {
-      hipLaunchKernelGGL((residual_kernel<T, TPR, V>), dim3(min(p.M, 1 << 20)), dim3(TPR), 0, p.stream, p);
-      return hipGetLastError();
-    }
+    hipLaunchKernelGGL((residual_kernel<T, TPR, V>), dim3(min(p.M, 1 << 20)), dim3(TPR), 0, p.stream, p);
+    return hipGetLastError();
   });
 }
 
 template <typename T>
 hipError_t launch_bwd_t(const ResidualArgs& p) {
-  const Units un = units_of(p.M, p.gate_rows, p.dgate != nullptr);
+  const Units un = units_of(p.M, p.gate_rows, p.dgate != nullptr, threads_of(p.K, p.dtype));
   float* next = p.ws;
   auto take = [&](bool wanted) {
     float* q = wanted ? next : nullptr;
@@ -353,33 +460,29 @@ hipError_t launch_bwd_t(const ResidualArgs& p) {
   float* part_post = take(p.dg_post != nullptr);
   float* part_pre = take(p.dg_pre != nullptr);
   float* part_gate = take(p.dgate && un.pieces);
-  const hipError_t e = with_shape<T>(p.K, [&](auto tpr, auto v) {
-    constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value;
-    if constexpr (sizeof(T) == 2 && V > 2) return hipErrorInvalidValue;
-    else if (un.count) {
-      hipLaunchKernelGGL((residual_bwd_kernel<T, TPR, V>), dim3((unsigned)un.count), dim3(TPR), 0, p.stream, p, un,
-                         part_post, part_pre, part_gate);
-    }
-    return hipGetLastError();
-  });
-  if (e != hipSuccess) return e;
-  const unsigned cols = (p.K + 63) / 64;
-  if (p.dg_post)
-    hipLaunchKernelGGL(residual_reduce_kernel<float>, dim3(cols), dim3(1024), 0, p.stream, part_post, p.K, un.count,
-                       p.dg_post, (int64_t)p.K);
-  if (p.dg_pre)
-    hipLaunchKernelGGL(residual_reduce_kernel<float>, dim3(cols), dim3(1024), 0, p.stream, part_pre, p.K, un.count,
-                       p.dg_pre, (int64_t)p.K);
-  if (part_gate)
-    hipLaunchKernelGGL(residual_reduce_kernel<T>, dim3(cols, (unsigned)(un.count / un.pieces)), dim3(1024), 0, p.stream,
-                       part_gate, p.K, (int64_t)un.pieces, (T*)p.dgate, (int64_t)p.lddg);
+  if (un.count) {
+    const hipError_t e = with_shape<T>(p.K, [&](auto tpr, auto v) {
+      constexpr int TPR = decltype(tpr)::value, V = decltype(v)::value;
+      auto go = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, dim3((unsigned)un.count), dim3(TPR), 0, p.stream, p, un, part_post, part_pre, part_gate);
+        return hipGetLastError();
+      };
+      if (p.g_post) return p.g_pre ? go(residual_bwd_kernel<T, TPR, V, true, true>) : go(residual_bwd_kernel<T, TPR, V, true, false>);
+      return p.g_pre ? go(residual_bwd_kernel<T, TPR, V, false, true>) : go(residual_bwd_kernel<T, TPR, V, false, false>);
+    });
+    if (e != hipSuccess) return e;
+  }
+  const unsigned sums = (p.dg_post ? 1 : 0) + (p.dg_pre ? 1 : 0) + (part_gate ? (unsigned)(un.count / un.pieces) : 0);
+  if (!sums) return hipSuccess;
+  hipLaunchKernelGGL(residual_sums_kernel<T>, dim3((p.K + 31) / 32, sums), dim3(256), 0, p.stream, p, un, part_post, part_pre,
+                     part_gate);
   return hipGetLastError();
 }
 
 }  // namespace
 
-int64_t residual_bwd_ws_floats(int64_t M, int64_t K, int64_t gate_rows, int, bool post, bool pre, bool gate) {
-  const Units un = units_of(M, gate_rows, gate);
+int64_t residual_bwd_ws_floats(int64_t M, int64_t K, int64_t gate_rows, int dtype, bool post, bool pre, bool gate) {
+  const Units un = units_of(M, gate_rows, gate, threads_of(K, dtype));
   return un.count * K * ((post ? 1 : 0) + (pre ? 1 : 0) + (gate && un.pieces ? 1 : 0));
 }
 
