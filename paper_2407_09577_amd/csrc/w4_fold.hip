@@ -13,64 +13,166 @@ __device__ __forceinline__ double twelve_bits(double s) {
   return __longlong_as_double((long long)(u & ~((1ull << 41) - 1ull)));
 }
 
-// One wave quantises a code fragment: lane 16 c + p holds 32 k of column p, so a group's smallest and
-// largest product meet across the four lanes of a column.  g w is exact in fp64, the scale is rounded
-// once from it and the code is the nearest one to the fp64 quotient, so the result does not depend on
-// the order of anything.
+// A group's scale and zero point from its extremes.  R(span) below 2^-126 is 0, beyond fp32 NaN; then z = 8.
+__device__ __forceinline__ double w4_span(double lo, double hi, bool zero_points) {
+  return zero_points ? (hi - lo) / 15.0 : fmax(-lo, hi) / 7.0;
+}
+__device__ __forceinline__ void w4_scale_of(double lo, double hi, bool bad, bool zero_points, float& s, float& z) {
+  const double d = twelve_bits(w4_span(lo, hi, zero_points));
+  s = bad || !(d <= 0x1.fffffep127) ? __builtin_nanf("") : d < 0x1p-126 ? 0.0f : (float)d;
+  z = zero_points && s > 0.0f ? (float)fmin(fmax(rint(-lo / d), 0.0), 15.0) : 8.0f;
+}
+
+// A weight view and the position of a lane's 32 values in it: k0 + 32 u + e.
+template <typename T>
+struct W4Source {
+  const T* W;
+  int64_t sk, sn, K, n, k0;
+  const float* g;
+  bool vec, gvec;
+  // Eight products g w, rounded to fp32; zeros past K.
+  __device__ __forceinline__ void products(int u, float (&p)[8]) const {
+    float gv[8];
+    load_k8(W, sk, sn, k0 + 32 * u, n, K, vec, p);
+    load_v8(g, k0 + 32 * u, K, gvec, 1.0f, gv);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] *= gv[e];
+  }
+  // One product, exactly.
+  __device__ __forceinline__ double exact(int u, int e) const {
+    const int64_t k = k0 + 32 * u + e;
+    if (n < 0 || k >= K) return 0.0;
+    return (double)widen(W[k * sk + n * sn]) * (g ? (double)g[k] : 1.0);
+  }
+};
+
+__device__ __forceinline__ void w4_put(u32x4& out, int u, int e, unsigned q) {
+  const unsigned shift = w4_bit(e);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) out[i] = i == u ? (out[i] & ~(15u << shift)) | q << shift : out[i];
+}
+
+// One wave quantises a code fragment: lane 16 c + p holds 32 k of column p, so a group's smallest and largest
+// product meet across the four lanes of a column.  By definition g w is exact, the scale is rounded once from
+// the extremes and the code is the nearest one to the fp64 quotient, so the result does not depend on the order
+// of anything.  fp32 decides the same nearly always:
+//   the extremes and the span are off by at most 2^-24 of themselves, so the scale is the exact one's unless a
+//   border between twelve-bit values lies that near (one group in 1000: the products that round to the extremes
+//   are taken again in fp64);
+//   a quotient (at most 16) is off by 3 * 2^-24 of itself, less than 2^-18, so its nearest whole number is the
+//   right one unless it is that near to a half (one weight in 130000: decided again in fp64).
+// Groups whose largest product is not between 2^-100 and 2^100 are taken in fp64 throughout, but for zeros.
+// Bound by memory and, nearly as much, by the arithmetic: about ten operations a weight.  4096 x 22016 bf16 from
+// [N, K]: 114 us with fp64 quotients throughout.
 template <typename T, int GB>
 __global__ __launch_bounds__(256) void w4_fold_kernel(const T* __restrict__ W, int64_t sk, int64_t sn, int64_t K,
                                                       int64_t N, const float* __restrict__ g, int glu, bool vec,
                                                       bool gvec, bool zero_points, int NPB, int KB, int kgroups,
                                                       u32x4* __restrict__ codes, unsigned* __restrict__ scales) {
+  constexpr int NG = 4 / GB;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane >> 4;
   const int cq = blockIdx.x / kgroups, kq = blockIdx.x % kgroups;
   const int cb = sk == 1 ? cq : 4 * cq + wave, kb = sk == 1 ? 4 * kq + wave : kq;
   if (cb >= NPB || kb >= KB) return;
-  const int64_t n = logical_col((int64_t)cb * 16 + (lane & 15), N, glu);
-  float w[4][8], gv[4][8];
+  const W4Source<T> src{W, sk, sn, K, logical_col((int64_t)cb * 16 + (lane & 15), N, glu), (int64_t)kb * kW4KB + 8 * c, g,
+                        vec, gvec};
+  float p[4][8], s[NG], z[NG], low[NG], high[NG];
 #pragma unroll
-  for (int u = 0; u < 4; ++u) load_k8(W, sk, sn, (int64_t)kb * kW4KB + 32 * u + 8 * c, n, K, vec, w[u]);
+  for (int u = 0; u < 4; ++u) src.products(u, p[u]);
+  bool near = false, far = false;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) load_v8(g, (int64_t)kb * kW4KB + 32 * u + 8 * c, K, gvec, 1.0f, gv[u]);
-  u32x4 out;
+  for (int j = 0; j < NG; ++j) {
+    float lo = 0.0f, hi = 0.0f, any = 0.0f;
 #pragma unroll
-  for (int u0 = 0; u0 < 4; u0 += GB) {
-    double lo = 0.0, hi = 0.0;
-    bool bad = false;
+    for (int u = j * GB; u < (j + 1) * GB; ++u)
 #pragma unroll
-    for (int u = u0; u < u0 + GB; ++u)
+      for (int e = 0; e < 8; e += 2) {
+        lo = fminf(fminf(lo, p[u][e]), p[u][e + 1]);
+        hi = fmaxf(fmaxf(hi, p[u][e]), p[u][e + 1]);
+        any += p[u][e] + p[u][e + 1];  // NaN where a product is: the extremes skip it
+      }
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const double t = n >= 0 ? (double)gv[u][e] * (double)w[u][e] : 0.0;
+    for (int o = 16; o <= 32; o <<= 1) {
+      lo = fminf(lo, __shfl_xor(lo, o));
+      hi = fmaxf(hi, __shfl_xor(hi, o));
+      any += __shfl_xor(any, o);
+    }
+    low[j] = lo, high[j] = hi;
+    const double span = w4_span(lo, hi, zero_points);
+    const float top = fmaxf(-lo, hi), q = zero_points ? lo / (float)span : 0.0f;
+    w4_scale_of(lo, hi, false, zero_points, s[j], z[j]);
+    far |= any != any || !(top == 0.0f || (top >= 0x1p-100f && top <= 0x1p100f));
+    near |= top > 0.0f && (twelve_bits(span * (1.0 - 0x1p-23)) != twelve_bits(span * (1.0 + 0x1p-23)) ||
+                           fabsf(q - rintf(q)) > 0.5f - 0x1p-12f);  // q from the unrounded span: 2^-12 off
+  }
+  if (__any(near | far)) {
+#pragma unroll
+    for (int j = 0; j < NG; ++j) {
+      // Rounding keeps the order: the exact extremes are among the products that round to the extremes.
+      unsigned at = far ? 0xffffffffu : 0;
+#pragma unroll
+      for (int u = j * GB; u < (j + 1) * GB; ++u)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (p[u][e] == low[j] || p[u][e] == high[j]) at |= 1u << (8 * u + e);
+      if constexpr (GB < 4) at &= ((1u << (8 * (GB & 3))) - 1u) << (8 * GB * j);
+      double lo = 0.0, hi = 0.0;
+      bool bad = false;
+      while (at) {
+        const int i = __builtin_ctz(at);
+        at &= at - 1;
+        const double t = src.exact(i >> 3, i & 7);
         lo = fmin(lo, t);
         hi = fmax(hi, t);
         bad |= !(fabs(t) <= 0x1p300);
       }
 #pragma unroll
-    for (int o = 16; o <= 32; o <<= 1) {
-      lo = fmin(lo, __shfl_xor(lo, o));
-      hi = fmax(hi, __shfl_xor(hi, o));
-      bad |= __shfl_xor((int)bad, o) != 0;
-    }
-    double s = twelve_bits(zero_points ? (hi - lo) / 15.0 : fmax(-lo, hi) / 7.0);
-    if (s < 0x1p-126) s = 0.0;
-    if (!(s <= 0x1.fffffep127) || bad) s = __builtin_nan("");
-    double z = 8.0;
-    if (zero_points && s > 0.0) z = fmin(fmax(rint(-lo / s), 0.0), 15.0);
-#pragma unroll
-    for (int u = u0; u < u0 + GB; ++u) {
-      unsigned word = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const double t = n >= 0 ? (double)gv[u][e] * (double)w[u][e] : 0.0;
-        const double q = s > 0.0 ? fmin(fmax(rint(t / s) + z, 0.0), 15.0) : z;
-        word |= (unsigned)(int)q << w4_bit(e);
+      for (int o = 16; o <= 32; o <<= 1) {
+        lo = fmin(lo, __shfl_xor(lo, o));
+        hi = fmax(hi, __shfl_xor(hi, o));
+        bad |= __shfl_xor((int)bad, o) != 0;
       }
-      out[u] = word;
+      w4_scale_of(lo, hi, bad, zero_points, s[j], z[j]);
     }
-    if (lane < 16)
-      scales[((int64_t)kb * (4 / GB) + u0 / GB) * NPB * 16 + cb * 16 + lane] =
-          (__float_as_uint((float)s) & kW4ScaleMask) | (unsigned)(int)z;
+  }
+  u32x4 out;
+  unsigned again = 0;  // bit 8 u + e: the code is to be decided in fp64
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const float sj = s[u / GB], zj = z[u / GB], inv = sj > 0.0f ? 1.0f / sj : 0.0f;
+    float q[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float t = p[u][e] * inv, r = rintf(t);
+      if (fabsf(t - r) > 0.5f - 0x1p-18f) again |= 1u << (8 * u + e);
+      q[e] = r + zj;
+      if (zero_points) q[e] = fminf(q[e], 15.0f);  // without them |r| is at most 7
+    }
+    // Codes to bytes (below zero: zero), even nibbles and odd ones.
+    unsigned even = 0, odd = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = 4 * (i & 1) + (i >> 1);  // bytes 0..3: codes 0, 4, 1, 5; and 2, 6, 3, 7
+      even = __builtin_amdgcn_cvt_pk_u8_f32(q[e], i, even);
+      odd = __builtin_amdgcn_cvt_pk_u8_f32(q[e + 2], i, odd);
+    }
+    out[u] = even | odd << 4;
+  }
+  if (far) again = 0xffffffffu;
+  while (again) {
+    const int i = __builtin_ctz(again), u = i >> 3, e = i & 7;
+    again &= again - 1;
+    float sj = s[0], zj = z[0];
+#pragma unroll
+    for (int j = 1; j < NG; ++j)
+      if (u / GB == j) sj = s[j], zj = z[j];
+    const double q = sj > 0.0f ? fmin(fmax(rint(src.exact(u, e) / (double)sj) + (double)zj, 0.0), 15.0) : (double)zj;
+    w4_put(out, u, e, (unsigned)(int)q);
+  }
+  if (lane < 16) {
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
+      scales[((int64_t)kb * NG + j) * NPB * 16 + cb * 16 + lane] = (__float_as_uint(s[j]) & kW4ScaleMask) | (unsigned)z[j];
   }
   codes[((int64_t)kb * NPB + cb) * 64 + lane] = out;
 }
