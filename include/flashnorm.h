@@ -438,7 +438,8 @@ int unpack_weights_w4(const void* W4, int64_t K, int64_t N, int layout, int grou
                       int64_t ldo, void* stream);
 
 /* Bytes of workspace that a product of M rows with a logical [K, N] weight of the layout needs
- * (0 for few rows, and for invalid arguments).  Host only. */
+ * (0 for few rows, up to FN_W4_FEW_M always, and for invalid arguments).  Host only. */
+#define FN_W4_FEW_M 16
 size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout);
 
 /* flashnorm_linear, flashnorm_glu and rowscale_linear with a 4-bit weight.  Sums are fp32.  Few

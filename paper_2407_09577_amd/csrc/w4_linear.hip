@@ -1,4 +1,5 @@
 // Products with 4-bit weights: which kernel and workgroup shape of w4_kernels.h a call takes, and its launches.
+#include "flashnorm.h"
 #include "w4_kernels.h"
 
 namespace fn {
@@ -63,7 +64,7 @@ static W4Plan w4_plan(int M, int K, int KB, int NP, bool glu) {
       const float us = kW4FewUs + kW4FewPerMK * mk + shape_us(s, wgs, (KB + s.ks - 1) / s.ks);
       if (us < best_us) best_us = us, best = W4Plan{false, i, 1, KB};
     }
-    if (M <= 16) return best;
+    if (M <= FN_W4_FEW_M) return best;
   }
   for (int i = 0; i < (int)(sizeof(kW4Many) / sizeof(W4Shape)); ++i) {
     const W4Shape& s = kW4Many[i];
