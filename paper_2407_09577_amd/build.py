@@ -1,8 +1,10 @@
-"""Build ``libflashnorm.so`` (gfx950) in-tree with hipcc.
+"""Build ``libflashnorm.so`` (gfx950) in-tree with hipcc, and the Python entry points on top of it.
 
 Every ``csrc/*.hip`` file is compiled for gfx950 only, in parallel, then linked
 into one shared library next to this file.  Packed-fp32 VALU instructions are
 disabled for all device code (the kernels use scalar fp32 arithmetic).
+``csrc/binding.cpp`` (host code, against the installed torch) becomes the extension
+module ``_binding`` beside it.
 """
 from __future__ import annotations
 
@@ -11,6 +13,7 @@ import glob
 import os
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -18,7 +21,9 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libflashnorm.so")
+BINDING_PATH = os.path.join(HERE, "_binding.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+CXX = os.environ.get("CXX", "g++")
 ARCH = "gfx950"
 
 CFLAGS = [
@@ -37,19 +42,48 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _compile_binding() -> str:
+    import torch
+    from torch.utils import cpp_extension
+    src, obj = os.path.join(CSRC, "binding.cpp"), os.path.join(BUILD_DIR, "binding.cpp.o")
+    paths = [*cpp_extension.include_paths("cuda"), sysconfig.get_paths()["include"], INCLUDE]
+    cmd = [CXX, "-O2", "-std=c++17", "-fPIC", "-fvisibility=hidden", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *(f"-isystem{p}" for p in paths), "-c", src,
+           "-o", obj]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"{CXX} failed for {src}:\n{r.stderr}")
+    return obj
+
+
+def _link_binding(obj: str) -> None:
+    import torch
+    libs = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = BINDING_PATH + f".tmp{os.getpid()}"
+    cmd = [CXX, "-shared", obj, f"-L{HERE}", "-l:libflashnorm.so", f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10",
+           "-lc10_hip", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{libs}", "-o", tmp]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"link failed:\n{r.stderr}")
+    os.replace(tmp, BINDING_PATH)
+
+
 def build(verbose: bool = True) -> str:
-    """Compile every HIP source and link the library; always rebuilds."""
+    """Compile every source and link the library and the binding; always rebuilds."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
-    workers = min(len(srcs), max(1, (os.cpu_count() or 4)), 8)
+    workers = min(len(srcs) + 1, max(1, (os.cpu_count() or 4)), 8)
     with cf.ThreadPoolExecutor(max_workers=workers) as ex:
+        binding = ex.submit(_compile_binding)
         objs = list(ex.map(_compile, srcs))
+        binding_obj = binding.result()
     tmp = LIB_PATH + f".tmp{os.getpid()}"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
     os.replace(tmp, LIB_PATH)
+    _link_binding(binding_obj)
     if verbose:
         print(f"built {LIB_PATH} from {len(srcs)} sources", file=sys.stderr)
     return LIB_PATH

@@ -23,6 +23,7 @@ FN_LAYOUT_LINEAR, FN_LAYOUT_GLU = 0, 1
 FN_PATH_AUTO, FN_PATH_PREFILL, FN_PATH_DECODE = 0, 1, 2
 FN_DECODE_MAX_M = 16
 FN_W4_FEW_M = 16  # up to this many rows a 4-bit product needs no workspace
+BINDING_PATH = os.path.join(HERE, "_binding.so")
 FN_GLU_SWIGLU, FN_GLU_REGLU, FN_GLU_BILINEAR, FN_GLU_SWIGLU_DEFER_UP = 0, 1, 2, 3
 
 STATUS = {0: "FN_OK", -1: "FN_ERR_NULL", -2: "FN_ERR_SHAPE", -3: "FN_ERR_DTYPE", -4: "FN_ERR_ALIGN",
@@ -30,6 +31,7 @@ STATUS = {0: "FN_OK", -1: "FN_ERR_NULL", -2: "FN_ERR_SHAPE", -3: "FN_ERR_DTYPE",
           -9: "FN_ERR_SIZE"}
 
 _lib = None
+_binding = None
 
 
 class FlashNormError(RuntimeError):
@@ -543,10 +545,6 @@ def _current_device():
     return _raw_device() if _raw_device else torch.cuda.current_device()
 
 
-def _stream_of(dev):
-    return _raw_stream(dev) if _raw_stream else torch.cuda.current_stream(dev).cuda_stream
-
-
 def _elsewhere(t, stream):
     d = t.get_device()
     return stream is not None or d < 0 or d != _current_device()
@@ -647,148 +645,51 @@ def unpack_weights_w4(w4: W4Weight, stream=None) -> torch.Tensor:
     return out
 
 
-@functools.lru_cache(maxsize=4096)
-def _w4_workspace(M, K, N, layout):  # a pure function of the four, asked again by every call
-    return _load().flashnorm_w4_workspace_size(M, K, N, layout)
+def binding():
+    """The compiled entry points of the calls below (csrc/binding.cpp): they check the tensors, allocate what the
+    caller does not pass and call the C ABI on the current stream, in a third of the time that this takes in
+    Python (one row of 4096 through the block residual: 8.5 us a call before, 4.2 so, 3.4 of them the launch)."""
+    global _binding
+    if _binding is None:
+        _load()
+        if not os.path.exists(BINDING_PATH):
+            raise RuntimeError(f"{BINDING_PATH} is not built: run `python -c 'import __graft_entry__ as g; g.build()'`")
+        from . import _binding as module
+        _binding = module
+    return _binding
 
 
-def _workspace(where, workspace, need, like):
-    """The caller's workspace, checked, or a new one; None where none is needed."""
-    if not need:
-        return None
-    if workspace is None:
-        return torch.empty(need, dtype=torch.uint8, device=like.device)
-    if workspace.get_device() != like.get_device() or not workspace.is_contiguous() or \
-            workspace.numel() * workspace.element_size() < need:
-        raise ValueError(f"{where}: the workspace must be {need} contiguous bytes on {like.device}")
-    return workspace
-
-
-# The calls below run beside kernels of a few microseconds: they look at what they are given with as few
-# queries as it takes, and at what is absent with none (16 x 4096 -> 6144: 7.6 us a call with the checks in
-# helpers, {T1} so, 3.4 of them the launch).
-_CODE = {torch.bfloat16: FN_BF16, torch.float32: FN_F32}
-
-
-def _refuse_dtype(t):
-    raise TypeError(f"unsupported dtype {t.dtype}")
-
-
-def _row_pitch(t):
-    s = t.stride()
-    if s[1] != 1 and t.shape[1] > 1:
-        raise ValueError("expected a row-major 2-D tensor (unit column stride)")
-    return s[0] if t.shape[0] > 1 else max(s[0], t.shape[1])  # one row's pitch says nothing
-
-
-def _vec_ptr(where, t, n, name, dev):
-    if t.dtype != torch.float32 or t.numel() != n or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous fp32 vector of {n} elements")
-    if t.get_device() != dev:
-        raise ValueError(f"{where}: tensors on cuda:{dev} and {t.device}; all must be on one GPU")
-    return t.data_ptr()
-
-
-def _mat_ptr(where, t, shape, dtype, dev, name):
-    if t.shape != shape or t.dtype != dtype:
-        raise ValueError(f"{where}: {name} of shape {tuple(t.shape)}, {t.dtype}, expected {tuple(shape)}, {dtype}")
-    if t.get_device() != dev:
-        raise ValueError(f"{where}: tensors on cuda:{dev} and {t.device}; all must be on one GPU")
-    return t.data_ptr()
-
-
-def _new_rows(like, M, N, per):
-    """A new [M, N] beside like, its rows padded to `per` elements (16 bytes)."""
-    if N % per or type(like) is not torch.Tensor:
-        return _new_out(M, N, like)
-    return like.new_empty(M, N)
-
-
-def _w4_operands(where, a, w4, layout, N, out, workspace, dev):
-    """Checks of a product's operands: M, K, the type code, the output, the workspace and its size."""
-    M, K = a.shape
-    data = w4.data
-    if K != w4.K or layout != w4.layout:
-        raise ValueError(f"{where}: activations of width {K}, layout {layout}, and a 4-bit weight of K = {w4.K}, "
-                         f"layout {w4.layout}")
-    if data.get_device() != dev:
-        raise ValueError(f"{where}: tensors on cuda:{dev} and {data.device}; all must be on one GPU")
-    dtype = a.dtype
-    code = _CODE.get(dtype)
-    if code is None:
-        _refuse_dtype(a)
-    if out is None:
-        out = _new_rows(a, M, N, 8 if code == FN_BF16 else 4)
-    else:
-        _mat_ptr(where, out, (M, N), dtype, dev, "an output")
-    need, ws = 0, None
-    if M > FN_W4_FEW_M:
-        need = _w4_workspace(M, K, w4.N, layout)
-        if need:
-            ws = _workspace(where, workspace, need, a).data_ptr()
-    return M, K, code, out, ws, need
+def _call(where, name, first, stream, *args):
+    """The compiled entry point `name`, on the asked stream and the GPU of the tensor `first`."""
+    entry = getattr(_binding or binding(), name)
+    r = entry(*args) if stream is None else None
+    if r is None:  # another stream, or another GPU than the current one
+        with _current(where, first, stream):
+            r = entry(*args)
+    if type(r) is int:
+        raise FlashNormError(r, where)
+    return r
 
 
 def flashnorm_linear_w4(a: torch.Tensor, w4: W4Weight, eps: float, g=None, bias=None, out=None, inv_rms=None,
                         workspace=None, stream=None) -> torch.Tensor:
     """y = RMSNorm(a) W4 (+ bias), deferred; g: the norm weight, where it is not folded into w4."""
-    where = "flashnorm_linear_w4"
-    dev = a.get_device()
-    if stream is not None or dev < 0 or dev != _current_device():
-        with _current(where, a, stream):
-            return flashnorm_linear_w4(a, w4, eps, g, bias, out, inv_rms, workspace)
-    N = w4.N
-    M, K, code, y, ws, need = _w4_operands(where, a, w4, FN_LAYOUT_LINEAR, N, out, workspace, dev)
-    status = _load().flashnorm_linear_w4(
-        a.data_ptr(), M, K, _row_pitch(a), code, None if g is None else _vec_ptr(where, g, K, "g", dev), w4.data.data_ptr(),
-        N, w4.group, eps, None if bias is None else _vec_ptr(where, bias, N, "bias", dev), y.data_ptr(), _row_pitch(y),
-        code, None if inv_rms is None else _vec_ptr(where, inv_rms, M, "inv_rms", dev), ws, need, _stream_of(dev))
-    if status:
-        raise FlashNormError(status, where)
-    return y
+    return _call("flashnorm_linear_w4", "w4_product", a, stream, 0, a, w4.data, w4.K, w4.N, w4.layout, w4.group, eps, g,
+                 bias, out, inv_rms, None, workspace)
 
 
 def flashnorm_glu_w4(a: torch.Tensor, w4: W4Weight, eps: float, g=None, out=None, workspace=None,
                      stream=None) -> torch.Tensor:
     """silu(RMSNorm(a) Wg) * (RMSNorm(a) Wu) with w4 = [Wg | Wu] (FN_LAYOUT_GLU)."""
-    where = "flashnorm_glu_w4"
-    dev = a.get_device()
-    if stream is not None or dev < 0 or dev != _current_device():
-        with _current(where, a, stream):
-            return flashnorm_glu_w4(a, w4, eps, g, out, workspace)
-    F = w4.N // 2
-    M, K, code, o, ws, need = _w4_operands(where, a, w4, FN_LAYOUT_GLU, F, out, workspace, dev)
-    status = _load().flashnorm_glu_w4(
-        a.data_ptr(), M, K, _row_pitch(a), code, None if g is None else _vec_ptr(where, g, K, "g", dev), w4.data.data_ptr(),
-        F, w4.group, eps, o.data_ptr(), _row_pitch(o), code, ws, need, _stream_of(dev))
-    if status:
-        raise FlashNormError(status, where)
-    return o
+    return _call("flashnorm_glu_w4", "w4_product", a, stream, 1, a, w4.data, w4.K, w4.N, w4.layout, w4.group, eps, g, None,
+                 out, None, None, workspace)
 
 
 def rowscale_linear_w4(x: torch.Tensor, w4: W4Weight, row_scale=None, out=None, workspace=None,
                        stream=None) -> torch.Tensor:
     """y = (x W4) * row_scale[m], or x W4: a down projection, with a deferred norm's scale or without."""
-    where = "rowscale_linear_w4"
-    dev = x.get_device()
-    if stream is not None or dev < 0 or dev != _current_device():
-        with _current(where, x, stream):
-            return rowscale_linear_w4(x, w4, row_scale, out, workspace)
-    N = w4.N
-    M, K, code, y, ws, need = _w4_operands(where, x, w4, FN_LAYOUT_LINEAR, N, out, workspace, dev)
-    status = _load().rowscale_linear_w4(
-        x.data_ptr(), M, K, _row_pitch(x), code, w4.data.data_ptr(), N, w4.group,
-        None if row_scale is None else _vec_ptr(where, row_scale, M, "row_scale", dev), y.data_ptr(), _row_pitch(y), code,
-        ws, need, _stream_of(dev))
-    if status:
-        raise FlashNormError(status, where)
-    return y
-
-
-def _gate_ptr(where, gate, rows_per_gate, M, K, dtype, dev):
-    if rows_per_gate < 1:
-        raise ValueError(f"{where}: rows_per_gate must be at least 1")
-    return _mat_ptr(where, gate, (-(-M // rows_per_gate), K), dtype, dev, f"a gate for {M} rows, {rows_per_gate} to each,")
+    return _call("rowscale_linear_w4", "w4_product", x, stream, 2, x, w4.data, w4.K, w4.N, w4.layout, w4.group, 0.0, None,
+                 None, out, None, row_scale, workspace)
 
 
 def flashnorm_block_residual(x: torch.Tensor, h: torch.Tensor, g_post=None, eps_post: float = 0.0, gate=None,
@@ -796,45 +697,8 @@ def flashnorm_block_residual(x: torch.Tensor, h: torch.Tensor, g_post=None, eps_
                              eps_pre: float = 0.0, out=None, normed=None, inv_rms=None, stream=None):
     """out = res_scale h + branch_scale gate RMSNorm(x; g_post), normed = RMSNorm(out; g_pre).  Returns
     (out, normed); normed is None without g_pre.  out may be h, normed may be x."""
-    where = "flashnorm_block_residual"
-    dev = x.get_device()
-    if stream is not None or dev < 0 or dev != _current_device():
-        with _current(where, x, stream):
-            return flashnorm_block_residual(x, h, g_post, eps_post, gate, rows_per_gate, res_scale, branch_scale, g_pre,
-                                            eps_pre, out, normed, inv_rms)
-    M, K = shape = x.shape
-    dtype = x.dtype
-    code = _CODE.get(dtype)
-    if code is None:
-        _refuse_dtype(x)
-    hp = _mat_ptr(where, h, shape, dtype, dev, "h")
-    if out is None:
-        out = _new_rows(x, M, K, 8 if code == FN_BF16 else 4)
-    elif out is not h:
-        _mat_ptr(where, out, shape, dtype, dev, "out")
-    if g_pre is not None:
-        if normed is None:
-            normed = _new_rows(x, M, K, 8 if code == FN_BF16 else 4)
-        elif normed is not x:
-            _mat_ptr(where, normed, shape, dtype, dev, "normed")
-    elif normed is not None:
-        raise ValueError(f"{where}: normed needs g_pre")
-    status = _load().flashnorm_block_residual(
-        x.data_ptr(), _row_pitch(x), hp, _row_pitch(h), M, K, code,
-        None if g_post is None else _vec_ptr(where, g_post, K, "g_post", dev), eps_post,
-        None if gate is None else _gate_ptr(where, gate, rows_per_gate, M, K, dtype, dev),
-        0 if gate is None else _row_pitch(gate), rows_per_gate, res_scale, branch_scale,
-        None if g_pre is None else _vec_ptr(where, g_pre, K, "g_pre", dev), eps_pre, out.data_ptr(), _row_pitch(out),
-        None if normed is None else normed.data_ptr(), 0 if normed is None else _row_pitch(normed),
-        None if inv_rms is None else _vec_ptr(where, inv_rms, M, "inv_rms", dev), _stream_of(dev))
-    if status:
-        raise FlashNormError(status, where)
-    return out, normed
-
-
-@functools.lru_cache(maxsize=4096)
-def _bwd_workspace(M, K, rows_per_gate, code):
-    return _load().flashnorm_block_residual_bwd_size(M, K, rows_per_gate, code)
+    return _call("flashnorm_block_residual", "block_residual", x, stream, x, h, g_post, eps_post, gate, rows_per_gate,
+                 res_scale, branch_scale, g_pre, eps_pre, out, normed, inv_rms)
 
 
 def flashnorm_block_residual_bwd(x: torch.Tensor, h: torch.Tensor, dh_out, dn=None, g_post=None, eps_post: float = 0.0,
@@ -842,35 +706,5 @@ def flashnorm_block_residual_bwd(x: torch.Tensor, h: torch.Tensor, dh_out, dn=No
                                  g_pre=None, eps_pre: float = 0.0, workspace=None, stream=None):
     """Gradients of flashnorm_block_residual from those at out (dh_out, None: zeros) and normed (dn, with
     g_pre).  Returns (dx, dh, dgate, dg_post, dg_pre), None for what the call has not."""
-    where = "flashnorm_block_residual_bwd"
-    dev = x.get_device()
-    if stream is not None or dev < 0 or dev != _current_device():
-        with _current(where, x, stream):
-            return flashnorm_block_residual_bwd(x, h, dh_out, dn, g_post, eps_post, gate, rows_per_gate, res_scale,
-                                                branch_scale, g_pre, eps_pre, workspace)
-    M, K = shape = x.shape
-    dtype = x.dtype
-    code = _CODE.get(dtype)
-    if code is None:
-        _refuse_dtype(x)
-    per = 8 if code == FN_BF16 else 4
-    mat = lambda t, name: None if t is None else _mat_ptr(where, t, shape, dtype, dev, name)
-    hp, dop, dnp = mat(h, "h"), mat(dh_out, "dh_out"), mat(dn, "dn")
-    post = None if g_post is None else _vec_ptr(where, g_post, K, "g_post", dev)
-    pre = None if g_pre is None else _vec_ptr(where, g_pre, K, "g_pre", dev)
-    gp = None if gate is None else _gate_ptr(where, gate, rows_per_gate, M, K, dtype, dev)
-    need = _bwd_workspace(M, K, 0 if gate is None else rows_per_gate, code)
-    ws = _workspace(where, workspace, need, x)
-    dx, dh = _new_rows(x, M, K, per), _new_rows(x, M, K, per)
-    dgate = None if gate is None else _new_rows(x, gate.shape[0], K, per)
-    sums = x.new_empty(2, K, dtype=torch.float32) if post and pre else None
-    dpost = sums[0] if sums is not None else g_post.new_empty(K) if post else None
-    dpre = sums[1] if sums is not None else g_pre.new_empty(K) if pre else None
-    pitch = lambda t: 0 if t is None else _row_pitch(t)
-    status = _load().flashnorm_block_residual_bwd(
-        x.data_ptr(), _row_pitch(x), hp, _row_pitch(h), dop, pitch(dh_out), dnp, pitch(dn), M, K, code, post, eps_post, gp,
-        pitch(gate), rows_per_gate, res_scale, branch_scale, pre, eps_pre, dx.data_ptr(), _row_pitch(dx), dh.data_ptr(),
-        _row_pitch(dh), _ptr(dgate), pitch(dgate), _ptr(dpost), _ptr(dpre), _ptr(ws), need, _stream_of(dev))
-    if status:
-        raise FlashNormError(status, where)
-    return dx, dh, dgate, dpost, dpre
+    return _call("flashnorm_block_residual_bwd", "block_residual_bwd", x, stream, x, h, dh_out, dn, g_post, eps_post, gate,
+                 rows_per_gate, res_scale, branch_scale, g_pre, eps_pre, workspace)
