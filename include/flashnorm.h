@@ -437,15 +437,15 @@ int pack_weights_w4(const uint8_t* codes, int64_t ldc, const float* scales, int6
 int unpack_weights_w4(const void* W4, int64_t K, int64_t N, int layout, int group, float* out,
                       int64_t ldo, void* stream);
 
-/* Bytes of workspace that a product of M rows with a logical [K, N] weight of the layout needs
- * (0 for few rows, up to FN_W4_FEW_M always, and for invalid arguments).  Host only. */
+/* Bytes of workspace that a product of M rows with such a weight needs, with a run-time g or
+ * without (0 for few rows, up to FN_W4_FEW_M always, and for invalid arguments).  Host only. */
 #define FN_W4_FEW_M 16
-size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout);
+size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout, int group);
 
 /* flashnorm_linear, flashnorm_glu and rowscale_linear with a 4-bit weight.  Sums are fp32.  Few
  * rows multiply the codes unrounded and scale a group's sum; many rows multiply a weight that is
  * rounded to 11 bits (at most 2^-11 of it, with its scale's rounding).  Which way a call goes
- * depends on M, K, N and the layout alone.
+ * depends on M, K, N, the layout, the group and the presence of g alone.
  *   a       [M, K] bf16 (fp32: FN_ERR_UNSUPPORTED), any M, K a multiple of 8.
  *   g       optional [K] fp32 norm weight applied at run time, for a weight into which none
  *           is folded.  a[m,k] g[k] enters the product with 11 bits or more (flashnorm_linear_unfolded

@@ -73,7 +73,7 @@ int run_w4(const W4Op& d) {
         (d.bias && overlaps(d.inv_rms, rbytes, d.bias, d.ncols * 4)))
       return FN_ERR_ALIAS;
   }
-  const int64_t NP = fn::packed_cols(N, d.glu), need = fn::w4_workspace(d.M, d.K, NP, d.glu);
+  const int64_t NP = fn::packed_cols(N, d.glu), need = fn::w4_workspace(d.M, d.K, NP, d.glu, d.group, d.g != nullptr);
   if (need > 0) {
     if (!d.ws) return FN_ERR_NULL;
     if (!aligned16(d.ws)) return FN_ERR_ALIGN;
@@ -156,10 +156,12 @@ int unpack_weights_w4(const void* W4, int64_t K, int64_t N, int layout, int grou
   return status_of(fn::launch_w4_unpack(W4, K, N, layout == FN_LAYOUT_GLU, group, out, ldo, (hipStream_t)stream));
 }
 
-size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout) {
-  if (M < 0 || M > kMaxRows || check_w4(K, N, layout, 128)) return 0;
+size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout, int group) {
+  if (M < 0 || M > kMaxRows || check_w4(K, N, layout, group)) return 0;
   const bool glu = layout == FN_LAYOUT_GLU;
-  return (size_t)fn::w4_workspace(M, K, fn::packed_cols(N, glu), glu);
+  const int64_t NP = fn::packed_cols(N, glu), plain = fn::w4_workspace(M, K, NP, glu, group, false);
+  const int64_t with_g = fn::w4_workspace(M, K, NP, glu, group, true);  // either call fits
+  return (size_t)(plain > with_g ? plain : with_g);
 }
 
 int flashnorm_linear_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype, const float* g, const void* W4,

@@ -185,7 +185,7 @@ PyObject* w4_product(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const Tensor* out = tensor_or_none(v[10]);
     float* inv_rms = vector(c, tensor_or_none(v[11]), M, "inv_rms");
     const float* row_scale = vector(c, tensor_or_none(v[12]), M, "row_scale");
-    const size_t need = M > FN_W4_FEW_M ? flashnorm_w4_workspace_size(M, K, N, (int)layout) : 0;
+    const size_t need = M > FN_W4_FEW_M ? flashnorm_w4_workspace_size(M, K, N, (int)layout, (int)group) : 0;
     const Tensor ws = workspace(c, tensor_or_none(v[13]), need, a);
     const Tensor made = out ? Tensor() : new_matrix(c, a, M, cols);
     const Matrix Y = matrix(c, out ? out : &made, M, cols, "the output");

@@ -194,7 +194,7 @@ struct W4Args {
 };
 // hipErrorInvalidConfiguration: more workgroups than a launch takes.
 hipError_t launch_w4(const W4Args& p);
-int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu);
+int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu, int group, bool gs);
 
 // Block residual (residual.hip).
 struct ResidualArgs {

@@ -37,10 +37,14 @@ __device__ __forceinline__ void split_ag(const bf16x8& a, const f32x4& g0, const
   }
 }
 
-// Few rows (M <= 16): bound by the weight stream.  A workgroup owns NCB column blocks; its KS waves take
-// sets of U code blocks (128 k each) in turn, the next set's loads in flight while the present one is
-// multiplied, and the partial products meet in LDS in a fixed order.
-template <int NCB, int KS, int U, int GB, int EPI, bool GS>
+// Few rows: bound by the weight stream.  A workgroup owns 16 rows and NCB column blocks; its KS waves take sets
+// of U code blocks (128 k each) in turn, the next set's loads in flight while the present one is multiplied, and
+// the partial products meet in LDS in a fixed order.
+// A wave's activations come straight in the matrix-core order, where sixteen rows lie in one load, or STAGED: read
+// along the rows and turned in a slot of LDS of its own.  That halves the requests of a load of sixteen rows
+// (4096 -> 6144 with one column block a wave: 11.9 -> 9.1 us) and only adds a wait to one of a row or two
+// (two blocks: 6.6 -> 7.6).
+template <int NCB, int KS, int U, int GB, int EPI, bool GS, bool STAGED>
 __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restrict__ a, int M, int K, int lda,
                                                          const void* __restrict__ codes,
                                                          const unsigned* __restrict__ scales, int NP, int KB, int ncols,
@@ -48,7 +52,11 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
   constexpr bool kSS = epi_needs_ss(EPI);
   constexpr int NG = 4 / GB, STEP = epi_is_glu(EPI) ? 2 : 1;
   static_assert(NCB % STEP == 0, "GLU needs gate/up block pairs");
-  __shared__ f32x4 red[KS][NCB][64];
+  // Each wave's slot for a block's activations, then (behind a barrier) the partial products.
+  static_assert(STAGED || !GS, "a g is split on its way through LDS");
+  constexpr int PLANES = GS ? 2 : 1, SLOT = STAGED ? 256 * PLANES : 0;  // units of a wave's slot
+  constexpr int UNITS = KS * (SLOT > 64 * NCB ? SLOT : 64 * NCB);
+  __shared__ u32x4 smem[UNITS];
   __shared__ float red_ss[KS][16];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -69,7 +77,7 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
   const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{one2, one2, one2, one2});
 
   struct Set {
-    u32x4 w[U][NCB], a[U][4];
+    u32x4 w[U][NCB], a[U][4], g[U][GS ? 2 : 1];
     unsigned s[U][NG][NCB];
   };
   auto load_set = [&](int kb0, Set& t) __attribute__((always_inline)) {
@@ -87,19 +95,53 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
           t.s[i][j][c] = __builtin_amdgcn_raw_buffer_load_b32(
               rs_s, ok ? (unsigned)((kb * NG + j) * NP + (cb0 + c) * 16 + lrow) * 4u : kOobOffset, 0, 0);
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int k = kb * kW4KB + 32 * u + 8 * lch;
-        t.a[i][u] = load_buf16(rs_a, lrow < rows && k < K ? (unsigned)(lrow * lda + k) * 2 : kOobOffset);
+      for (int j = 0; j < 4; ++j) {
+        // Staged: sixteen lanes read one row's 256 bytes, four rows at a time.  Else: the matrix-core order.
+        const int row = STAGED ? 4 * j + lch : lrow, k = kb * kW4KB + (STAGED ? 8 * lrow : 32 * j + 8 * lch);
+        if (GS && 4 * j >= rows) continue;  // what a row costs is its splitting (else the branch costs more)
+        t.a[i][j] = load_buf16(rs_a, row < rows && k < K ? (unsigned)(row * lda + k) * 2 : kOobOffset);
+      }
+      if constexpr (GS) {  // this lane's eight k, the same for its four rows; past K: zeros
+        const unsigned k = (unsigned)(kb * kW4KB + 8 * lrow);
+        t.g[i][0] = load_buf16(rs_g, k * 4);
+        t.g[i][1] = load_buf16(rs_g, k * 4 + 16);
       }
     }
   };
+  // Piece (k block u, chunk c) of row r in the slot: where the matrix-core order reads it, at a position XORed
+  // so that the sixteen pieces of a row are written to different banks.
+  auto slot = [](int u, int r, int c) { return u * 64 + 16 * c + (r ^ (c + 4 * u)); };
+  u32x4* own = smem + wave * SLOT;
+  if constexpr (GS) {
+    if (rows <= 12) {
+#pragma unroll
+      for (int i = 0; i < SLOT / 64; ++i) own[i * 64 + lane] = u32x4{0, 0, 0, 0};
+    }
+  }
   f32x4 acc[NCB];
 #pragma unroll
   for (int c = 0; c < NCB; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float ss = 0.f;
-  auto compute_set = [&](int kb0, const Set& t) __attribute__((always_inline)) {
+  float ss = 0.f, ss4[4] = {0.f, 0.f, 0.f, 0.f};  // GS: of the raw rows 4 j + lch
+  auto compute_set = [&](const Set& t) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < U; ++i) {
+      if constexpr (STAGED) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if (GS && 4 * j >= rows) continue;  // the slot holds zeros there
+          const int at = slot(lrow >> 2, 4 * j + lch, lrow & 3);
+          if constexpr (GS) {
+            bf16x8 hi, lo;
+            if constexpr (kSS) ss4[j] = sumsq8(__builtin_bit_cast(bf16x8, t.a[i][j]), ss4[j]);
+            split_ag(__builtin_bit_cast(bf16x8, t.a[i][j]), __builtin_bit_cast(f32x4, t.g[i][0]),
+                     __builtin_bit_cast(f32x4, t.g[i][1]), hi, lo);
+            own[at] = __builtin_bit_cast(u32x4, hi);
+            own[256 + at] = __builtin_bit_cast(u32x4, lo);
+          } else {
+            own[at] = t.a[i][j];
+          }
+        }
+      }
 #pragma unroll
       for (int j = 0; j < NG; ++j) {
         bf16x8 av[GB], al[GB];
@@ -107,12 +149,10 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
 #pragma unroll
         for (int b = 0; b < GB; ++b) {
           const int u = j * GB + b;
-          av[b] = __builtin_bit_cast(bf16x8, t.a[i][u]);
-          if constexpr (kSS) ss = sumsq8(av[b], ss);
+          av[b] = __builtin_bit_cast(bf16x8, STAGED ? own[slot(u, lrow, lch)] : t.a[i][u]);
+          if constexpr (kSS && !GS) ss = sumsq8(av[b], ss);
           if constexpr (GS) {
-            const unsigned k = (unsigned)((kb0 + i * KS) * kW4KB + 32 * u + 8 * lch);  // past K: zeros
-            split_ag(av[b], __builtin_bit_cast(f32x4, load_buf16(rs_g, k * 4)),
-                     __builtin_bit_cast(f32x4, load_buf16(rs_g, k * 4 + 16)), av[b], al[b]);
+            al[b] = __builtin_bit_cast(bf16x8, own[256 + slot(u, lrow, lch)]);
             sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al[b], ones, sum, 0, 0, 0);
           }
           sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[b], ones, sum, 0, 0, 0);
@@ -138,29 +178,38 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
   for (int kb0 = wave; kb0 < KB; kb0 += 2 * U * KS) {
     load_set(kb0 + U * KS, t1);
     __builtin_amdgcn_sched_barrier(0);
-    compute_set(kb0, t0);
+    compute_set(t0);
     __builtin_amdgcn_sched_barrier(0);
     if (kb0 + U * KS >= KB) break;
     load_set(kb0 + 2 * U * KS, t0);
     __builtin_amdgcn_sched_barrier(0);
-    compute_set(kb0 + U * KS, t1);
+    compute_set(t1);
     __builtin_amdgcn_sched_barrier(0);
   }
 
-  if constexpr (kSS) {
+  if constexpr (kSS && GS) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+#pragma unroll
+      for (int o = 1; o < 16; o <<= 1) ss4[j] += __shfl_xor(ss4[j], o);
+      if (lrow == 0) red_ss[wave][4 * j + lch] = ss4[j];
+    }
+  } else if constexpr (kSS) {
     ss += __shfl_xor(ss, 16);
     ss += __shfl_xor(ss, 32);
     if (lane < 16) red_ss[wave][lane] = ss;
   }
+  __syncthreads();
+  f32x4* red = reinterpret_cast<f32x4*>(smem);
 #pragma unroll
-  for (int c = 0; c < NCB; ++c) red[wave][c][lane] = acc[c];
+  for (int c = 0; c < NCB; ++c) red[(wave * NCB + c) * 64 + lane] = acc[c];
   __syncthreads();
   for (int o = wave; o < NCB / STEP; o += KS) {
-    f32x4 v = red[0][o * STEP][lane], u = red[0][o * STEP + STEP - 1][lane];
+    f32x4 v = red[o * STEP * 64 + lane], u = red[(o * STEP + STEP - 1) * 64 + lane];
 #pragma unroll
     for (int w = 1; w < KS; ++w) {
-      v += red[w][o * STEP][lane];
-      if constexpr (STEP == 2) u += red[w][o * STEP + 1][lane];
+      v += red[(w * NCB + o * STEP) * 64 + lane];
+      if constexpr (STEP == 2) u += red[(w * NCB + o * STEP + 1) * 64 + lane];
     }
     const int n = (cb0 / STEP + o) * 16 + lrow;
     const float bias = EPI == EPI_RMS && ep.bias && n < ncols ? ep.bias[n] : 0.0f;
@@ -354,18 +403,14 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
   // Transfer i of a wave: rows (i NW + wave) 4 .. + 3 of the set's KS x ROWS rows of 256 bytes.  Rows past M
   // and blocks past the split's end bring zeros: their offsets lie beyond the extent, which is below 2^30.
   constexpr unsigned kPast = 0x60000000u;
-  unsigned a_off[ND];
-#pragma unroll
-  for (int i = 0; i < ND; ++i) {
-    const int row4 = (i * NW + wave) * 4, j = row4 / ROWS, r = row4 % ROWS + lch;
-    const unsigned off = (unsigned)(r * p.KP + j * kW4KB) * 2u + (unsigned)((lrow ^ (r & 15)) * 16);
-    a_off[i] = r < rows ? off : kOobOffset;
-  }
+  static_assert(ROWS % (4 * NW) == 0, "a wave's rows are 4 NW apart, in one k group after the other");
+  const unsigned a_off = (unsigned)((wave * 4 + lch) * p.KP) * 2u + (unsigned)((lrow ^ ((wave * 4 + lch) & 15)) * 16);
   auto load_act = [&](int kb0, int st) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
-      const int row4 = (i * NW + wave) * 4, kb = kb0 + row4 / ROWS;
-      load_lds16(rs_a, smem + st * STAGE + row4 * 256, a_off[i] + (kb < kb_end ? (unsigned)kb0 * (2 * kW4KB) : kPast));
+      const int row4 = (i * NW + wave) * 4, j = i * NW * 4 / ROWS;
+      const unsigned at = (unsigned)(i * NW * 4 % ROWS * p.KP + (kb0 + j) * kW4KB) * 2u;
+      load_lds16(rs_a, smem + st * STAGE + row4 * 256, a_off + (kb0 + j < kb_end ? at : kPast));
     }
   };
   struct Weights {
@@ -399,22 +444,30 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
   const int rbase = (kg * ROWS + wm * MB * 16 + lrow) * 256;
   auto compute = [&](int st, const Weights& t) __attribute__((always_inline)) {
     const char* stage = smem + st * STAGE + rbase;
-    f16x2 zero[NG][NCB], r[NG][NCB];
+    auto zero_of = [&](int j, int c) __attribute__((always_inline)) {
+      const unsigned z = t.s[j][c] & 63u;
+      return __builtin_bit_cast(f16x2, 0x64006400u + (z | z << 16));
+    };
+    auto scale_of = [&](int j, int c) __attribute__((always_inline)) {
+      const _Float16 h = (_Float16)(w4_scale(t.s[j][c]) * norm[c]);
+      return f16x2{h, h};
+    };
+    // Kept over the k blocks that share them; with a group per k block they are made where they are used
+    // (held ahead they cost 32 registers, and the 128 x 256 shape spilled its sums).
+    f16x2 zero[NG < 4 ? NG : 1][NCB], r[NG < 4 ? NG : 1][NCB];
+    if constexpr (NG < 4) {
 #pragma unroll
-    for (int j = 0; j < NG; ++j)
+      for (int j = 0; j < NG; ++j)
 #pragma unroll
-      for (int c = 0; c < NCB; ++c) {
-        const unsigned z = t.s[j][c] & 63u;
-        zero[j][c] = __builtin_bit_cast(f16x2, 0x64006400u + (z | z << 16));
-        const _Float16 h = (_Float16)(w4_scale(t.s[j][c]) * norm[c]);
-        r[j][c] = f16x2{h, h};
-      }
+        for (int c = 0; c < NCB; ++c) zero[j][c] = zero_of(j, c), r[j][c] = scale_of(j, c);
+    }
     // Steps of one row block of one k block of 32: its operand is read D steps ahead, and the next k block's
     // weights are widened between the steps.
     constexpr int STEPS = 4 * MB, D = STEPS < 4 ? STEPS : 4, WPS = (NCB + MB - 1) / MB;
     f16x8 wv[2][NCB], av[D];
     auto widen = [&](int u, int c) __attribute__((always_inline)) {
-      const f16x2 z1 = zero[u / GB][c], r1 = r[u / GB][c];
+      const f16x2 z1 = NG < 4 ? zero[NG < 4 ? u / GB : 0][c] : zero_of(u / GB, c);
+      const f16x2 r1 = NG < 4 ? r[NG < 4 ? u / GB : 0][c] : scale_of(u / GB, c);
       // 1024 + 16 z = 16 (1024 + z) - 15 * 1024, exactly
       const f16x2 z16 = (z1 - f16x2{1024, 1024}) * f16x2{16, 16} + f16x2{1024, 1024};
       wv[u & 1][c] = w4_widen_f16(t.w[c][u], z1, z16, r1, r1 * f16x2{0.0625, 0.0625});
@@ -580,12 +633,20 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Gemm p) {
   }
 }
 
+// Rows from which the activations are staged: at 5 x 11008 -> 4096 the two are within 4% of each other.
+constexpr int kW4StagedM = 6;
+
 template <int NCB, int KS, int GB, int EPI, bool GS>
 static hipError_t launch_w4_few_cfg(const W4Args& p) {
   const int tiles = (p.NP / 16 + NCB - 1) / NCB, groups = (p.M + 15) / 16;
-  hipLaunchKernelGGL((w4_few_kernel<NCB, KS, 1, GB, EPI, GS>), dim3((unsigned)tiles * groups), dim3(64 * KS), 0,
-                     p.stream, p.a, p.M, p.K, p.lda, p.codes, p.scales, p.NP, p.KB, p.ncols, p.y, p.ldy, p.ep, groups);
-  return hipGetLastError();
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)tiles * groups), dim3(64 * KS), 0, p.stream, p.a, p.M, p.K, p.lda, p.codes,
+                       p.scales, p.NP, p.KB, p.ncols, p.y, p.ldy, p.ep, groups);
+    return hipGetLastError();
+  };
+  if constexpr (!GS)
+    if (p.M < kW4StagedM) return go(w4_few_kernel<NCB, KS, 1, GB, EPI, GS, false>);
+  return go(w4_few_kernel<NCB, KS, 1, GB, EPI, GS, true>);
 }
 
 // The shapes of w4_linear.hip's kW4Few, in its order.

@@ -16,27 +16,27 @@ extern template hipError_t launch_w4_many<EPI_ROWSCALE>(const W4Gemm&, int, int,
 //   start ceil(r / per_cu) + sets (full (ceil(r / per_cu) - 1) + last) + each r,
 // `last` going from one to full as the last round fills up.  Beside it stand what the kernel's launches cost
 // (kW4FewUs, kW4ManyUs), the activations' pass and, with splits of K, the join of their sums.  The constants
-// are least-squares fits over 500 (few rows: 1..200 rows) and 400 (17..2048 rows) random shapes of K 256..11008
+// are least-squares fits over 900 (few rows: 1..200 rows) and 400 (17..2048 rows) random shapes of K 256..11008
 // and 256..22016 columns, linear and GLU, groups of 128, each shape's weights read in turn from 400 MB: 7%
-// rms for the many-row shapes and 10 to 17% for the few-row ones, whose times are launches in large part.  The
-// shape so chosen took 0.7% (many rows) and 3% (few) more than the best of each call.
+// rms for the many-row shapes and 8 to 12% for the few-row ones, whose times are launches in large part.  The
+// shape so chosen took 0.7% (many rows) and 1.7% (few) more than the best of each call, in the mean.
 struct W4Shape {
   int rows, cols, ks, per_cu;
   float start, full, one, each;
 };
 static constexpr W4Shape kW4Few[] = {
-    {16, 32, 8, 2, 0.497f, 1.648f, 0.629f, 0.0f},   {16, 64, 8, 2, 0.510f, 2.514f, 1.137f, 0.0f},
-    {16, 96, 8, 2, 0.0f, 3.959f, 1.652f, 0.815f},   {16, 128, 8, 1, 0.0f, 3.032f, 2.159f, 0.827f},
-    {16, 64, 4, 4, 0.269f, 2.534f, 0.905f, 0.107f}, {16, 32, 4, 4, 0.351f, 1.710f, 0.593f, 0.0f},
-    {16, 16, 8, 2, 0.333f, 1.206f, 0.552f, 0.0f},   {16, 16, 16, 1, 0.113f, 1.506f, 1.072f, 0.0f},
-    {16, 48, 8, 2, 0.619f, 1.946f, 0.886f, 0.007f}};
+    {16, 32, 8, 2, 0.894f, 1.359f, 0.642f, 0.0f},   {16, 64, 8, 2, 0.510f, 2.930f, 1.183f, 0.431f},
+    {16, 96, 8, 2, 0.098f, 4.176f, 1.694f, 1.151f}, {16, 128, 8, 1, 0.0f, 2.924f, 2.265f, 1.162f},
+    {16, 64, 4, 4, 0.376f, 2.450f, 1.010f, 0.195f}, {16, 32, 4, 4, 0.734f, 1.431f, 0.644f, 0.0f},
+    {16, 16, 8, 2, 0.901f, 0.942f, 0.437f, 0.0f},   {16, 16, 16, 1, 0.430f, 1.177f, 0.930f, 0.0f},
+    {16, 48, 8, 2, 0.795f, 1.849f, 0.899f, 0.040f}};
 static constexpr W4Shape kW4Many[] = {
     {128, 256, 1, 2, 2.783f, 2.873f, 1.827f, 1.490f}, {128, 128, 1, 2, 1.119f, 1.671f, 1.054f, 1.610f},
     {96, 256, 1, 2, 1.981f, 2.361f, 1.526f, 1.524f},  {96, 128, 1, 3, 0.646f, 1.884f, 0.868f, 1.465f},
     {64, 128, 2, 2, 0.339f, 2.016f, 1.175f, 1.665f},  {64, 128, 1, 4, 0.010f, 1.909f, 0.710f, 1.254f},
     {32, 128, 2, 4, 0.0f, 3.001f, 0.873f, 1.052f},    {32, 64, 4, 2, 0.0f, 1.835f, 0.998f, 0.877f}};
 constexpr int kW4FewLinearOnly = 6;  // from here on: single column blocks hold no gate/up pairs
-constexpr float kW4FewUs = 4.43f, kW4FewPerMK = 1.59f;
+constexpr float kW4FewUs = 3.89f, kW4FewPerMK = 1.01f;
 constexpr float kW4ManyUs = 7.69f, kW4ManyPerMK = 0.945f, kW4JoinUs = 2.43f, kW4JoinPerMB = 0.287f;
 // The few-row kernel reads its rows once per column tile and is not looked at beyond this many.
 constexpr int kW4FewMaxM = 256;
@@ -53,7 +53,11 @@ struct W4Plan {
   int shape, splits, kb_per_split;
 };
 
-static W4Plan w4_plan(int M, int K, int KB, int NP, bool glu) {
+// Smaller groups and a run-time g cost the few-row kernel most: a scale, a sum and four multiply-adds per group and
+// column, and two matrix-core operations for one.  Measured at 16..128 rows as factors of the shapes' times.
+static W4Plan w4_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs) {
+  const float few_x = (group == 32 ? 1.55f : group == 64 ? 1.2f : 1.0f) * (gs ? 1.9f : 1.0f);
+  const float many_x = group == 32 ? 1.15f : group == 64 ? 1.04f : 1.0f;
   W4Plan best{false, 0, 1, KB};
   float best_us = 1e30f;
   const float mk = (float)M * (float)K * 1e-6f;
@@ -61,7 +65,7 @@ static W4Plan w4_plan(int M, int K, int KB, int NP, bool glu) {
     for (int i = 0; i < (glu ? kW4FewLinearOnly : (int)(sizeof(kW4Few) / sizeof(W4Shape))); ++i) {
       const W4Shape& s = kW4Few[i];
       const int64_t wgs = (int64_t)((M + 15) / 16) * ((NP + s.cols - 1) / s.cols);
-      const float us = kW4FewUs + kW4FewPerMK * mk + shape_us(s, wgs, (KB + s.ks - 1) / s.ks);
+      const float us = kW4FewUs + kW4FewPerMK * mk + few_x * shape_us(s, wgs, (KB + s.ks - 1) / s.ks);
       if (us < best_us) best_us = us, best = W4Plan{false, i, 1, KB};
     }
     if (M <= FN_W4_FEW_M) return best;
@@ -72,7 +76,7 @@ static W4Plan w4_plan(int M, int K, int KB, int NP, bool glu) {
     for (int splits = 1; splits <= 16; splits *= 2) {
       if (splits > 1 && (tiles * splits > 1100 || KB < 2 * splits)) break;
       const int per = ((KB + splits - 1) / splits + s.ks - 1) / s.ks * s.ks, n = (KB + per - 1) / per;
-      float us = kW4ManyUs + kW4ManyPerMK * mk + shape_us(s, tiles * n, per / s.ks);
+      float us = kW4ManyUs + kW4ManyPerMK * mk + many_x * shape_us(s, tiles * n, per / s.ks);
       if (n > 1) us += kW4JoinUs + kW4JoinPerMB * (float)n * (float)M * (float)NP * 4e-6f;
       if (us < best_us) best_us = us, best = W4Plan{true, i, n, per};
     }
@@ -87,9 +91,9 @@ static int64_t w4_ws(const W4Plan& plan, int64_t M, int64_t KB, int64_t NP) {
   return factor_bytes(M) + M * KB * (2 * kW4KB) + (plan.splits > 1 ? plan.splits * M * NP * 4 : 0);
 }
 
-int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu) {
+int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu, int group, bool gs) {
   const int KB = (int)w4_blocks(K);
-  return M > 0 ? w4_ws(w4_plan((int)M, (int)K, KB, (int)NP, glu), M, KB, NP) : 0;
+  return M > 0 ? w4_ws(w4_plan((int)M, (int)K, KB, (int)NP, glu, group, gs), M, KB, NP) : 0;
 }
 
 template <bool NORM>
@@ -108,7 +112,7 @@ static hipError_t launch_w4_rows(const W4Args& p, _Float16* out, float* factor) 
 
 hipError_t launch_w4(const W4Args& p) {
   const bool glu = epi_is_glu(p.epi);
-  const W4Plan plan = w4_plan(p.M, p.K, p.KB, p.NP, glu);
+  const W4Plan plan = w4_plan(p.M, p.K, p.KB, p.NP, glu, p.group, p.ep.g_rt != nullptr);
   const W4Shape& s = plan.many ? kW4Many[plan.shape] : kW4Few[plan.shape];
   const int64_t groups = (p.M + s.rows - 1) / s.rows, wgs = groups * ((p.NP + s.cols - 1) / s.cols) * plan.splits;
   // A launch has fewer than 2^32 threads; the pass over the rows has up to 1024 of them each.

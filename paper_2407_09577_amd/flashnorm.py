@@ -79,7 +79,7 @@ def _load():
         "fold_weights_w4": ([P, I64, I64, I, P, I64, I64, I, I, I, P, P], I),
         "pack_weights_w4": ([P, I64, P, I64, P, I64, I64, I64, I, I, P, P], I),
         "unpack_weights_w4": ([P, I64, I64, I, I, P, I64, P], I),
-        "flashnorm_w4_workspace_size": ([I64, I64, I64, I], ctypes.c_size_t),
+        "flashnorm_w4_workspace_size": ([I64, I64, I64, I, I], ctypes.c_size_t),
         "flashnorm_linear_w4": ([P, I64, I64, I64, I, P, P, I64, I, F, P, P, I64, I, P, P, ctypes.c_size_t, P], I),
         "flashnorm_glu_w4": ([P, I64, I64, I64, I, P, P, I64, I, F, P, I64, I, P, ctypes.c_size_t, P], I),
         "rowscale_linear_w4": ([P, I64, I64, I64, I, P, I64, I, P, P, I64, I, P, ctypes.c_size_t, P], I),

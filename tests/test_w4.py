@@ -351,7 +351,7 @@ def test_workspace(fn):
     K, N = 512, 320
     codes, scales, z = weights(K, N, 64, True, 11)
     w4 = fn.pack_weights_w4(codes.to(DEV), scales.to(DEV), z.to(DEV), group=64)
-    need = {M: fn.lib().flashnorm_w4_workspace_size(M, K, N, 0) for M in (1, 16, 300, 2000)}
+    need = {M: fn.lib().flashnorm_w4_workspace_size(M, K, N, 0, 64) for M in (1, 16, 300, 2000)}
     assert need[1] == need[16] == 0 and need[2000] > 2000 * K * 2
     ws = torch.full((max(need.values()) + 64,), 7, dtype=torch.uint8, device=DEV)
     for M in (2000, 300, 1, 2000):

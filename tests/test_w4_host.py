@@ -62,13 +62,14 @@ def test_products_refuse(lib):
     big = dict(M=1 << 30, K=8, lda=8, N=1 << 20, ldy=1 << 20, y=1 << 60)
     assert _lin(lib, ws=1 << 61, wb=1 << 59, **big) == -9   # more workgroups than a launch takes
     assert _lin(lib, M=1000) == -1                          # a workspace is needed
-    need = lib.flashnorm_w4_workspace_size(1000, 64, 32, 0)
+    need = lib.flashnorm_w4_workspace_size(1000, 64, 32, 0, 32)
     assert need > 1000 * 64 * 2
     assert _lin(lib, M=1000, ws=B, wb=need - 1) == -9
     assert _lin(lib, M=1000, ws=B + 8, wb=need) == -4
     assert _lin(lib, M=1000, ws=Y, wb=need) == -8 and _lin(lib, M=1000, ws=A, wb=need) == -8
     f = lib.flashnorm_w4_workspace_size
-    assert f(16, 4096, 4096, 0) == 0 and f(0, 64, 32, 0) == 0 and f(-1, 64, 32, 0) == 0 and f(1000, 64, 31, 1) == 0
+    assert f(16, 4096, 4096, 0, 128) == 0 and f(0, 64, 32, 0, 32) == 0 and f(-1, 64, 32, 0, 32) == 0
+    assert f(1000, 64, 31, 1, 32) == 0 and f(1000, 64, 32, 0, 16) == 0
     assert _lin(lib, M=0, a=0, y=0) == 0
     glu = lambda F=16, ldo=16, w=W: lib.flashnorm_glu_w4(A, 4, 64, 64, 1, None, w, F, 32, 1e-6, Y, ldo, 1, None, 0, None)
     assert glu(F=0) == -2 and glu(ldo=8) == -2 and glu(w=0) == -1
