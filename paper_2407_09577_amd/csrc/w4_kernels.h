@@ -644,7 +644,7 @@ static hipError_t launch_w4_few_cfg(const W4Args& p) {
                        p.scales, p.NP, p.KB, p.ncols, p.y, p.ldy, p.ep, groups);
     return hipGetLastError();
   };
-  if constexpr (!GS)
+  if constexpr (!GS && NCB < 8)
     if (p.M < kW4StagedM) return go(w4_few_kernel<NCB, KS, 1, GB, EPI, GS, false>);
   return go(w4_few_kernel<NCB, KS, 1, GB, EPI, GS, true>);
 }
@@ -656,7 +656,9 @@ static hipError_t launch_w4_few_g(const W4Args& p, int shape) {
     case 0: return launch_w4_few_cfg<2, 8, GB, EPI, GS>(p);
     case 1: return launch_w4_few_cfg<4, 8, GB, EPI, GS>(p);
     case 2: return launch_w4_few_cfg<6, 8, GB, EPI, GS>(p);
-    case 3: return launch_w4_few_cfg<8, 8, GB, EPI, GS>(p);
+    case 3:
+      if constexpr (!GS) return launch_w4_few_cfg<8, 8, GB, EPI, GS>(p);
+      break;
     case 4: return launch_w4_few_cfg<4, 4, GB, EPI, GS>(p);
     case 5: return launch_w4_few_cfg<2, 4, GB, EPI, GS>(p);
     default:

@@ -35,7 +35,8 @@ static constexpr W4Shape kW4Many[] = {
     {96, 256, 1, 2, 1.981f, 2.361f, 1.526f, 1.524f},  {96, 128, 1, 3, 0.646f, 1.884f, 0.868f, 1.465f},
     {64, 128, 2, 2, 0.339f, 2.016f, 1.175f, 1.665f},  {64, 128, 1, 4, 0.010f, 1.909f, 0.710f, 1.254f},
     {32, 128, 2, 4, 0.0f, 3.001f, 0.873f, 1.052f},    {32, 64, 4, 2, 0.0f, 1.835f, 0.998f, 0.877f}};
-constexpr int kW4FewLinearOnly = 6;  // from here on: single column blocks hold no gate/up pairs
+constexpr int kW4FewWide = 3;        // several row groups without a run-time g: elsewhere never the least time
+constexpr int kW4FewLinearOnly = 6;  // from here on: an odd number of column blocks holds no gate/up pairs
 constexpr float kW4FewUs = 3.89f, kW4FewPerMK = 1.01f;
 constexpr float kW4ManyUs = 7.69f, kW4ManyPerMK = 0.945f, kW4JoinUs = 2.43f, kW4JoinPerMB = 0.287f;
 // The few-row kernel reads its rows once per column tile and is not looked at beyond this many.
@@ -55,7 +56,7 @@ struct W4Plan {
 
 // Smaller groups and a run-time g cost the few-row kernel most: a scale, a sum and four multiply-adds per group and
 // column, and two matrix-core operations for one.  Measured at 16..128 rows as factors of the shapes' times.
-static W4Plan w4_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs) {
+W4Plan w4_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs) {
   const float few_x = (group == 32 ? 1.55f : group == 64 ? 1.2f : 1.0f) * (gs ? 1.9f : 1.0f);
   const float many_x = group == 32 ? 1.15f : group == 64 ? 1.04f : 1.0f;
   W4Plan best{false, 0, 1, KB};
@@ -64,6 +65,7 @@ static W4Plan w4_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs
   if (M <= kW4FewMaxM) {
     for (int i = 0; i < (glu ? kW4FewLinearOnly : (int)(sizeof(kW4Few) / sizeof(W4Shape))); ++i) {
       const W4Shape& s = kW4Few[i];
+      if (i == kW4FewWide && (gs || M <= FN_W4_FEW_M)) continue;
       const int64_t wgs = (int64_t)((M + 15) / 16) * ((NP + s.cols - 1) / s.cols);
       const float us = kW4FewUs + kW4FewPerMK * mk + few_x * shape_us(s, wgs, (KB + s.ks - 1) / s.ks);
       if (us < best_us) best_us = us, best = W4Plan{false, i, 1, KB};
@@ -115,8 +117,8 @@ hipError_t launch_w4(const W4Args& p) {
   const W4Plan plan = w4_plan(p.M, p.K, p.KB, p.NP, glu, p.group, p.ep.g_rt != nullptr);
   const W4Shape& s = plan.many ? kW4Many[plan.shape] : kW4Few[plan.shape];
   const int64_t groups = (p.M + s.rows - 1) / s.rows, wgs = groups * ((p.NP + s.cols - 1) / s.cols) * plan.splits;
-  // A launch has fewer than 2^32 threads; the pass over the rows has up to 1024 of them each.
-  if (wgs * 512 >= (int64_t(1) << 32) || (plan.many && (int64_t)p.M * 1024 >= (int64_t(1) << 32)))
+  // A launch has fewer than 2^32 threads: up to 1024 per workgroup, in the pass over the rows too.
+  if (wgs * 1024 >= (int64_t(1) << 32) || (plan.many && (int64_t)p.M * 1024 >= (int64_t(1) << 32)))
     return hipErrorInvalidConfiguration;
   if (!plan.many) {
     switch (p.epi) {
