@@ -704,6 +704,9 @@ static hipError_t launch_w4_many_g(const W4Gemm& q, int shape, hipStream_t strea
     case 5: return launch_w4_many_cfg<4, 2, 4, 1, GB, EPI>(q, stream);
     case 6: return launch_w4_many_cfg<2, 2, 4, 2, GB, EPI>(q, stream);
     case 7: return launch_w4_many_cfg<2, 2, 2, 4, GB, EPI>(q, stream);
+    case 8: return launch_w4_many_cfg<6, 2, 4, 2, GB, EPI>(q, stream);
+    case 9: return launch_w4_many_cfg<8, 2, 4, 2, GB, EPI>(q, stream);
+    case 10: return launch_w4_many_cfg<2, 2, 1, 8, GB, EPI>(q, stream);
   }
   return hipErrorInvalidValue;
 }

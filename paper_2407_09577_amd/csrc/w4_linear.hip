@@ -16,10 +16,13 @@ extern template hipError_t launch_w4_many<EPI_ROWSCALE>(const W4Gemm&, int, int,
 //   start ceil(r / per_cu) + sets (full (ceil(r / per_cu) - 1) + last) + each r,
 // `last` going from one to full as the last round fills up.  Beside it stand what the kernel's launches cost
 // (kW4FewUs, kW4ManyUs), the activations' pass and, with splits of K, the join of their sums.  The constants
-// are least-squares fits over 900 (few rows: 1..200 rows) and 400 (17..2048 rows) random shapes of K 256..11008
-// and 256..22016 columns, linear and GLU, groups of 128, each shape's weights read in turn from 400 MB: 7%
+// are least-squares fits over 900 (few rows: 1..200 rows) and 500 (17..2048 rows) random shapes of K 256..11008
+// and 256..22016 columns, linear and GLU, groups of 128, each shape's weights read in turn from 400 MB: 6%
 // rms for the many-row shapes and 8 to 12% for the few-row ones, whose times are launches in large part.  The
-// shape so chosen took 0.7% (many rows) and 1.7% (few) more than the best of each call, in the mean.
+// shape so chosen took 0.8% (many rows) and 1.7% (few) more than the best of each call, in the mean.
+// One workgroup of four waves leaves a compute unit's SIMDs a wave each, which neither hides its reads nor its
+// widening: where a call has no more than a workgroup for each, two or eight k groups do (695 x 3928 x 3520:
+// 42.4 us with 96 x 128 tiles, 35.2 with two k groups on each).
 struct W4Shape {
   int rows, cols, ks, per_cu;
   float start, full, one, each;
@@ -31,14 +34,16 @@ static constexpr W4Shape kW4Few[] = {
     {16, 16, 8, 2, 0.901f, 0.942f, 0.437f, 0.0f},   {16, 16, 16, 1, 0.430f, 1.177f, 0.930f, 0.0f},
     {16, 48, 8, 2, 0.795f, 1.849f, 0.899f, 0.040f}};
 static constexpr W4Shape kW4Many[] = {
-    {128, 256, 1, 2, 2.783f, 2.873f, 1.827f, 1.490f}, {128, 128, 1, 2, 1.119f, 1.671f, 1.054f, 1.610f},
-    {96, 256, 1, 2, 1.981f, 2.361f, 1.526f, 1.524f},  {96, 128, 1, 3, 0.646f, 1.884f, 0.868f, 1.465f},
-    {64, 128, 2, 2, 0.339f, 2.016f, 1.175f, 1.665f},  {64, 128, 1, 4, 0.010f, 1.909f, 0.710f, 1.254f},
-    {32, 128, 2, 4, 0.0f, 3.001f, 0.873f, 1.052f},    {32, 64, 4, 2, 0.0f, 1.835f, 0.998f, 0.877f}};
+    {128, 256, 1, 2, 3.834f, 3.102f, 1.939f, 1.011f}, {128, 128, 1, 2, 1.149f, 1.627f, 1.087f, 2.125f},
+    {96, 256, 1, 2, 2.860f, 2.324f, 1.520f, 1.548f},  {96, 128, 1, 3, 0.798f, 1.829f, 0.880f, 1.601f},
+    {64, 128, 2, 2, 0.327f, 1.964f, 1.165f, 1.769f},  {64, 128, 1, 4, 0.328f, 1.877f, 0.683f, 1.202f},
+    {32, 128, 2, 4, 0.0f, 2.856f, 0.857f, 1.097f},    {32, 64, 4, 2, 0.018f, 1.635f, 0.962f, 0.986f},
+    {96, 128, 2, 1, 0.946f, 1.464f, 1.368f, 2.698f},  {128, 128, 2, 1, 1.548f, 1.816f, 1.688f, 2.916f},
+    {32, 32, 8, 1, 0.051f, 1.638f, 1.187f, 1.483f}};
 constexpr int kW4FewWide = 3;        // several row groups without a run-time g: elsewhere never the least time
 constexpr int kW4FewLinearOnly = 6;  // from here on: an odd number of column blocks holds no gate/up pairs
 constexpr float kW4FewUs = 3.89f, kW4FewPerMK = 1.01f;
-constexpr float kW4ManyUs = 7.69f, kW4ManyPerMK = 0.945f, kW4JoinUs = 2.43f, kW4JoinPerMB = 0.287f;
+constexpr float kW4ManyUs = 7.15f, kW4ManyPerMK = 1.30f, kW4JoinUs = 2.99f, kW4JoinPerMB = 0.223f;
 // The few-row kernel reads its rows once per column tile and is not looked at beyond this many.
 constexpr int kW4FewMaxM = 256;
 

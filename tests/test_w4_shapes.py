@@ -36,21 +36,24 @@ FEW = [  # read straight from memory, then staged through LDS (kW4StagedM rows a
     (5, (2, 144, 4307), (1, 152, 40)), (5, (6, 144, 4199), (13, 152, 40)), (6, (1, 144, 41), None), (6, (6, 144, 41), None),
     (7, (1, 1056, 41), None), (7, (11, 1048, 41), None), (8, (1, 520, 8809), None), (8, (6, 520, 8225), None)]
 MANY = [  # in one pass, then with K split
-    (0, (582, 144, 18777), (580, 144, 19212)), (0, (99, 5336, 18277), (101, 9312, 8436)),
-    (1, (519, 152, 10894), (321, 152, 16834)), (1, (639, 5216, 775), (225, 4200, 2198)),
-    (2, (413, 144, 19982), (388, 144, 20404)), (2, (65, 8280, 8539), (67, 4136, 16468)),
-    (3, (261, 144, 6815), (385, 144, 4686)), (3, (1105, 7264, 66), (1219, 6488, 90)),
-    (4, (1350, 664, 650), (1425, 648, 650)), (4, (1259, 4920, 65), (593, 10336, 66)),
-    (5, (401, 144, 2446), (830, 144, 1164)), (5, (545, 7216, 65), (1180, 3192, 68)),
-    (6, (262, 152, 40), (286, 144, 40)), (6, (867, 2120, 66), (829, 2120, 66)),
-    (7, (263, 280, 41), (269, 264, 44)), (7, (276, 1632, 40), (270, 1624, 40))]
+    (0, (582, 144, 18777), (769, 144, 14346)), (0, (106, 9464, 8414), (101, 9312, 8436)),
+    (1, (329, 144, 17885), (321, 152, 16834)), (1, (102, 8240, 4819), (114, 4392, 8358)),
+    (2, (388, 144, 20475), (388, 144, 20404)), (2, (65, 8280, 8539), (65, 7240, 8574)),
+    (3, (81, 144, 21709), (84, 144, 20822)), (3, (1401, 8720, 65), (803, 10248, 138)),
+    (4, (803, 408, 1160), (300, 400, 3252)), (4, (717, 6232, 66), (685, 6320, 68)),
+    (5, (1430, 144, 658), (830, 144, 1164)), (5, (417, 6360, 130), (723, 9328, 68)),
+    (6, (262, 152, 40), (286, 144, 40)), (6, (370, 5304, 65), (356, 5144, 66)),
+    (7, (269, 264, 41), (258, 264, 42)), (7, (262, 3104, 42), (261, 3120, 42)),
+    (8, (65, 1056, 16867), (130, 648, 13058)), (8, (1163, 10456, 65), (1134, 10824, 70)),
+    (9, (99, 904, 18987), (98, 928, 19618)), (9, (114, 4120, 4671), (113, 4152, 4716)),
+    (10, (283, 520, 40), (262, 536, 42)), (10, (264, 9240, 40), (17, 10344, 44))]
 CALLS = [(False, i % 2 == 1, s, c, glu) for i, (s, *cs) in enumerate(FEW) for glu, c in enumerate(cs) if c] + \
         [(True, i % 2 == 1, s, c, glu) for i, (s, *cs) in enumerate(MANY) for glu, c in enumerate(cs) if c]
 
 
 @pytest.mark.parametrize("group", [32, 64, 128])
 def test_every_shape_has_its_calls(group):
-    assert {s for s, *_ in FEW} == set(range(9)) and {s for s, *_ in MANY} == set(range(8))
+    assert {s for s, *_ in FEW} == set(range(9)) and {s for s, *_ in MANY} == set(range(11))
     for many, split, shape, call, glu in CALLS:
         for gs in (False, True):
             if gs and not many and shape == 3:
