@@ -60,8 +60,8 @@ def _link_binding(obj: str) -> None:
     import torch
     libs = os.path.join(os.path.dirname(torch.__file__), "lib")
     tmp = BINDING_PATH + f".tmp{os.getpid()}"
-    cmd = [CXX, "-shared", obj, f"-L{HERE}", "-l:libflashnorm.so", f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-lc10",
-           "-lc10_hip", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{libs}", "-o", tmp]
+    cmd = [CXX, "-shared", obj, f"-L{HERE}", "-l:libflashnorm.so", f"-L{libs}", "-ltorch_python", "-ltorch_cpu", "-ltorch_hip",
+           "-lc10", "-lc10_hip", "-Wl,-rpath,$ORIGIN", f"-Wl,-rpath,{libs}", "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")

@@ -1,4 +1,4 @@
-// Python entry points of the 4-bit products and the block residual.  These calls run beside kernels of a few
+// Python entry points of the 4-bit weights and the block residual.  These calls run beside kernels of a few
 // microseconds, so their tensors are looked at here and not through Python: what the C ABI cannot see (devices,
 // dtypes, shapes, the sizes of buffers) is checked, outputs and workspaces that the caller does not pass are
 // allocated, and the C ABI is called on the current stream of the tensors' GPU.  A call whose GPU is not the
@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/hip/EmptyTensor.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -54,6 +55,18 @@ int64_t integer(PyObject* o) {
   return v;
 }
 
+int small(PyObject* o) {
+  const int64_t v = integer(o);
+  if (v != (int)v) throw std::invalid_argument("an integer is out of range");
+  return (int)v;
+}
+
+bool flag(PyObject* o) {
+  const int v = PyObject_IsTrue(o);
+  if (v < 0) throw TypeError("expected a truth value");
+  return v != 0;
+}
+
 float real(PyObject* o) {
   const double v = PyFloat_AsDouble(o);
   if (v == -1.0 && PyErr_Occurred()) throw TypeError("expected a number");
@@ -61,10 +74,16 @@ float real(PyObject* o) {
 }
 
 // Begin a call by its first tensor; false where its GPU is not the current one (or it is on no GPU).
-bool begin(Call& c, const char* where, const Tensor& t) {
+bool begin_any(Call& c, const char* where, const Tensor& t) {
   c.where = where;
   if (!t.is_cuda() || t.get_device() != c10::hip::current_device()) return false;
   c.dev = (c10::DeviceIndex)t.get_device();
+  return true;
+}
+
+// The same with a matrix whose type is the call's.
+bool begin(Call& c, const char* where, const Tensor& t) {
+  if (!begin_any(c, where, t)) return false;
   c.type = t.scalar_type();
   if (c.type == at::kBFloat16) c.code = FN_BF16, c.per = 8;
   else if (c.type == at::kFloat) c.code = FN_F32, c.per = 4;
@@ -101,17 +120,22 @@ float* vector(const Call& c, const Tensor* t, int64_t n, const char* name) {
   return t->data_ptr<float>();
 }
 
-// A new matrix beside `like`, its rows padded to 16 bytes (a view of the first columns where that pads).
-Tensor new_matrix(const Call& c, const Tensor& like, int64_t rows, int64_t cols) {
+// A new tensor on the call's GPU, straight from torch's allocator: the operator call around it takes as long.
+Tensor new_tensor(const Call& c, at::IntArrayRef size, at::ScalarType type) {
+  return Tensor(at::detail::empty_cuda(size, type, c10::Device(c10::kCUDA, c.dev), std::nullopt));
+}
+
+// A new matrix, its rows padded to 16 bytes (a view of the first columns where that pads).
+Tensor new_matrix(const Call& c, int64_t rows, int64_t cols) {
   const int64_t ld = (cols + c.per - 1) / c.per * c.per;
-  Tensor t = at::empty({rows, ld}, like.options());
+  const Tensor t = new_tensor(c, {rows, ld}, c.type);
   return ld == cols ? t : t.narrow(1, 0, cols);
 }
 
 // The caller's workspace, checked, or a new one.
-Tensor workspace(const Call& c, const Tensor* given, size_t need, const Tensor& like) {
+Tensor workspace(const Call& c, const Tensor* given, size_t need) {
   if (!need) return Tensor();
-  if (!given) return at::empty({(int64_t)need}, like.options().dtype(at::kByte));
+  if (!given) return new_tensor(c, {(int64_t)need}, at::kByte);
   same_gpu(c, *given);
   if (!given->is_contiguous() || given->nbytes() < need)
     c.refuse("the workspace must be " + std::to_string(need) + " contiguous bytes");
@@ -156,6 +180,48 @@ bool arity(Py_ssize_t n, Py_ssize_t want) {
   return false;
 }
 
+// The size of a 4-bit weight; refused where there is none of that shape.
+int64_t w4_bytes(const Call& c, int64_t K, int64_t N, int layout, int group) {
+  const size_t bytes = fold_weights_w4_size(K, N, layout, group);
+  if (!bytes)
+    c.refuse("no 4-bit weight of K = " + std::to_string(K) + ", N = " + std::to_string(N) + ", layout " +
+             std::to_string(layout) + ", group " + std::to_string(group));
+  return (int64_t)bytes;
+}
+
+// W, g, layout, group, zero_points -> the packed weight
+PyObject* w4_fold(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!arity(n, 5)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const Tensor& W = tensor(v[0]);
+    Call c;
+    if (!begin(c, "fold_weights_w4", W)) Py_RETURN_NONE;
+    const int64_t K = W.size(0), N = W.size(1);
+    const int layout = small(v[2]), group = small(v[3]);
+    const float* g = vector(c, tensor_or_none(v[1]), K, "g");
+    const Tensor data = new_tensor(c, {w4_bytes(c, K, N, layout, group)}, at::kByte);
+    const int s = fold_weights_w4(W.data_ptr(), W.stride(0), W.stride(1), c.code, g, K, N, layout, group, flag(v[4]),
+                                  data.data_ptr(), stream_of(c));
+    return s ? PyLong_FromLong(s) : wrap(data);
+  });
+}
+
+// data, K, N, layout, group -> the fp32 weight
+PyObject* w4_unpack(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  if (!arity(n, 5)) return nullptr;
+  return guarded([&]() -> PyObject* {
+    const Tensor& data = tensor(v[0]);
+    Call c;
+    if (!begin_any(c, "unpack_weights_w4", data)) Py_RETURN_NONE;
+    const int64_t K = integer(v[1]), N = integer(v[2]);
+    const int layout = small(v[3]), group = small(v[4]);
+    if (!data.is_contiguous() || (int64_t)data.nbytes() < w4_bytes(c, K, N, layout, group)) c.refuse("no whole 4-bit weight");
+    const Tensor out = new_tensor(c, {K, N}, at::kFloat);
+    const int s = unpack_weights_w4(data.data_ptr(), K, N, layout, group, out.data_ptr<float>(), N, stream_of(c));
+    return s ? PyLong_FromLong(s) : wrap(out);
+  });
+}
+
 enum { kLinear, kGlu, kRowscale };
 
 // kind, a, data, K, N, layout, group, eps, g, bias, out, inv_rms, row_scale, workspace -> the output
@@ -169,15 +235,15 @@ PyObject* w4_product(PyObject*, PyObject* const* v, Py_ssize_t n) {
     Call c;
     if (!begin(c, names[kind], a)) Py_RETURN_NONE;
     const Tensor& data = tensor(v[2]);
-    const int64_t K = integer(v[3]), N = integer(v[4]), layout = integer(v[5]), group = integer(v[6]);
+    const int64_t K = integer(v[3]), N = integer(v[4]);
+    const int layout = small(v[5]), group = small(v[6]);
     const int want = kind == kGlu ? FN_LAYOUT_GLU : FN_LAYOUT_LINEAR;
     const int64_t M = a.size(0);
     if (a.size(1) != K || layout != want)
       c.refuse("activations of width " + std::to_string(a.size(1)) + " and layout " + std::to_string(want) +
                ", a 4-bit weight of K = " + std::to_string(K) + " and layout " + std::to_string(layout));
     same_gpu(c, data);
-    const size_t bytes = fold_weights_w4_size(K, N, (int)layout, (int)group);
-    if (!bytes || !data.is_contiguous() || data.nbytes() < bytes) c.refuse("no whole 4-bit weight");
+    if (!data.is_contiguous() || (int64_t)data.nbytes() < w4_bytes(c, K, N, layout, group)) c.refuse("no whole 4-bit weight");
     const int64_t cols = kind == kGlu ? N / 2 : N;
     const Matrix A = matrix(c, &a, M, K, "the activations");
     const float* g = vector(c, tensor_or_none(v[8]), K, "g");
@@ -185,20 +251,20 @@ PyObject* w4_product(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const Tensor* out = tensor_or_none(v[10]);
     float* inv_rms = vector(c, tensor_or_none(v[11]), M, "inv_rms");
     const float* row_scale = vector(c, tensor_or_none(v[12]), M, "row_scale");
-    const size_t need = M > FN_W4_FEW_M ? flashnorm_w4_workspace_size(M, K, N, (int)layout, (int)group) : 0;
-    const Tensor ws = workspace(c, tensor_or_none(v[13]), need, a);
-    const Tensor made = out ? Tensor() : new_matrix(c, a, M, cols);
+    const size_t need = M > FN_W4_FEW_M ? flashnorm_w4_workspace_size(M, K, N, layout, group) : 0;
+    const Tensor ws = workspace(c, tensor_or_none(v[13]), need);
+    const Tensor made = out ? Tensor() : new_matrix(c, M, cols);
     const Matrix Y = matrix(c, out ? out : &made, M, cols, "the output");
     const float eps = real(v[7]);
     int s;
     if (kind == kLinear)
-      s = flashnorm_linear_w4(A.p, M, K, A.ld, c.code, g, data.data_ptr(), N, (int)group, eps, bias, Y.p, Y.ld, c.code, inv_rms,
+      s = flashnorm_linear_w4(A.p, M, K, A.ld, c.code, g, data.data_ptr(), N, group, eps, bias, Y.p, Y.ld, c.code, inv_rms,
                               address(ws), need, stream_of(c));
     else if (kind == kGlu)
-      s = flashnorm_glu_w4(A.p, M, K, A.ld, c.code, g, data.data_ptr(), cols, (int)group, eps, Y.p, Y.ld, c.code, address(ws),
+      s = flashnorm_glu_w4(A.p, M, K, A.ld, c.code, g, data.data_ptr(), cols, group, eps, Y.p, Y.ld, c.code, address(ws),
                            need, stream_of(c));
     else
-      s = rowscale_linear_w4(A.p, M, K, A.ld, c.code, data.data_ptr(), N, (int)group, row_scale, Y.p, Y.ld, c.code, address(ws),
+      s = rowscale_linear_w4(A.p, M, K, A.ld, c.code, data.data_ptr(), N, group, row_scale, Y.p, Y.ld, c.code, address(ws),
                              need, stream_of(c));
     if (s) return PyLong_FromLong(s);
     return out ? again(v[10]) : wrap(made);
@@ -227,8 +293,8 @@ PyObject* block_residual(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const Tensor *out = tensor_or_none(v[10]), *normed = tensor_or_none(v[11]);
     if (normed && !g_pre) c.refuse("normed needs g_pre");
     float* inv_rms = vector(c, tensor_or_none(v[12]), M, "inv_rms");
-    const Tensor made = out ? Tensor() : new_matrix(c, x, M, K);
-    const Tensor made_n = normed || !g_pre ? Tensor() : new_matrix(c, x, M, K);
+    const Tensor made = out ? Tensor() : new_matrix(c, M, K);
+    const Tensor made_n = normed || !g_pre ? Tensor() : new_matrix(c, M, K);
     const Matrix O = matrix(c, out ? out : &made, M, K, "out");
     const Matrix NO = matrix(c, normed ? normed : made_n.defined() ? &made_n : nullptr, M, K, "normed");
     const int s = flashnorm_block_residual(X.p, X.ld, H.p, H.ld, M, K, c.code, g_post, real(v[3]), G.p, G.ld, rows_per_gate,
@@ -260,11 +326,11 @@ PyObject* block_residual_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const float* g_pre = vector(c, tensor_or_none(v[10]), K, "g_pre");
     const Matrix G = gate_of(c, gate, rows_per_gate, M, K);
     const size_t need = flashnorm_block_residual_bwd_size(M, K, gate ? rows_per_gate : 0, c.code);
-    const Tensor ws = workspace(c, tensor_or_none(v[12]), need, x);
-    const Tensor dx = new_matrix(c, x, M, K), dh = new_matrix(c, x, M, K);
-    const Tensor dgate = gate ? new_matrix(c, x, gate->size(0), K) : Tensor();
-    const auto f32 = x.options().dtype(at::kFloat);
-    const Tensor dpost = g_post ? at::empty({K}, f32) : Tensor(), dpre = g_pre ? at::empty({K}, f32) : Tensor();
+    const Tensor ws = workspace(c, tensor_or_none(v[12]), need);
+    const Tensor dx = new_matrix(c, M, K), dh = new_matrix(c, M, K);
+    const Tensor dgate = gate ? new_matrix(c, gate->size(0), K) : Tensor();
+    const Tensor dpost = g_post ? new_tensor(c, {K}, at::kFloat) : Tensor();
+    const Tensor dpre = g_pre ? new_tensor(c, {K}, at::kFloat) : Tensor();
     const Matrix DX = matrix(c, &dx, M, K, "dx"), DH = matrix(c, &dh, M, K, "dh");
     const Matrix DG = gate ? matrix(c, &dgate, gate->size(0), K, "dgate") : Matrix{};
     const int s = flashnorm_block_residual_bwd(
@@ -286,8 +352,12 @@ PyMethodDef method(const char* name) {
   return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(F)), METH_FASTCALL, nullptr};
 }
 
-PyMethodDef kMethods[] = {method<w4_product>("w4_product"), method<block_residual>("block_residual"),
-                          method<block_residual_bwd>("block_residual_bwd"), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef kMethods[] = {method<w4_fold>("w4_fold"),
+                          method<w4_unpack>("w4_unpack"),
+                          method<w4_product>("w4_product"),
+                          method<block_residual>("block_residual"),
+                          method<block_residual_bwd>("block_residual_bwd"),
+                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -597,16 +597,9 @@ def fold_weights_w4(W: torch.Tensor, g=None, layout: int = FN_LAYOUT_LINEAR, gro
                     zero_points: bool = False, stream=None) -> W4Weight:
     """Fold g into the logical [K, N] weight W (any strides; [Wg | Wu] for a GLU) and quantise it to
     4 bits with one scale (and zero point) per column and `group` consecutive k."""
-    if _elsewhere(W, stream):
-        with _current("fold_weights_w4", W, stream):
-            return fold_weights_w4(W, g, layout, group, zero_points)
-    if W.dim() != 2:
-        raise ValueError("W must be a 2-D [K, N] tensor")
-    K, N = W.shape
-    _on_gpu("fold_weights_w4", W, g)
-    w4 = _new_w4(K, N, layout, group, W.device)
-    _check(_load().fold_weights_w4(_ptr(W), W.stride(0), W.stride(1), _dt(W), _ptr(_vec(g, K, "g")), K, N, layout, group,
-                                   int(bool(zero_points)), _ptr(w4.data), _stream(None)), "fold_weights_w4")
+    data = _call("fold_weights_w4", "w4_fold", W, stream, W, g, layout, group, zero_points)
+    w4 = W4Weight.__new__(W4Weight)  # of the right size by construction
+    w4.data, (w4.K, w4.N), w4.layout, w4.group = data, W.shape, layout, group
     return w4
 
 
@@ -636,19 +629,14 @@ def pack_weights_w4(codes: torch.Tensor, scales: torch.Tensor, zeros=None, layou
 
 def unpack_weights_w4(w4: W4Weight, stream=None) -> torch.Tensor:
     """The logical [K, N] weight that w4 stands for, in fp32 (exact)."""
-    if _elsewhere(w4.data, stream):
-        with _current("unpack_weights_w4", w4.data, stream):
-            return unpack_weights_w4(w4)
-    out = torch.empty(w4.K, w4.N, dtype=torch.float32, device=w4.data.device)
-    _check(_load().unpack_weights_w4(_ptr(w4.data), w4.K, w4.N, w4.layout, w4.group, _ptr(out), w4.N, _stream(None)),
-           "unpack_weights_w4")
-    return out
+    return _call("unpack_weights_w4", "w4_unpack", w4.data, stream, w4.data, w4.K, w4.N, w4.layout, w4.group)
 
 
 def binding():
-    """The compiled entry points of the calls below (csrc/binding.cpp): they check the tensors, allocate what the
-    caller does not pass and call the C ABI on the current stream, in a third of the time that this takes in
-    Python (one row of 4096 through the block residual: 8.5 us a call before, 4.2 so, 3.4 of them the launch)."""
+    """The compiled entry points of the 4-bit weights and the block residual (csrc/binding.cpp): they check the
+    tensors, allocate what the caller does not pass and call the C ABI on the current stream, in a third of the
+    time that this takes in Python (one row of 4096 through the block residual: 8.5 us a call before, 3.9 so, 3.0
+    of them the launch)."""
     global _binding
     if _binding is None:
         _load()

@@ -429,3 +429,37 @@ def test_refusals_of_the_binding(fn):
         fn.fold_weights_w4(torch.ones(8, 7, device=DEV), layout=fn.FN_LAYOUT_GLU)
     with pytest.raises(ValueError):
         fn.W4Weight(w4.data[:-1], 64, 32, fn.FN_LAYOUT_LINEAR, 32)
+
+
+def test_refusals_of_the_fold(fn):
+    W = torch.ones(64, 32, device=DEV)
+    g = torch.ones(64, device=DEV)
+    for bad in (dict(g=g.cpu()), dict(g=g[:63]), dict(g=g.double()), dict(group=48), dict(group=(1 << 32) + 32), dict(layout=2),
+                dict(layout=1 << 32)):
+        with pytest.raises(ValueError):
+            fn.fold_weights_w4(W, **bad)
+    for W2 in (W[0], W.cpu(), W[:0], W[None]):
+        with pytest.raises(ValueError):
+            fn.fold_weights_w4(W2)
+    with pytest.raises(TypeError):
+        fn.fold_weights_w4(W.half())
+    with pytest.raises(TypeError):
+        fn.fold_weights_w4(W, group="32")
+    w4 = fn.fold_weights_w4(W, zero_points=np.bool_(True), group=32)
+    assert (w4.K, w4.N, w4.layout, w4.group) == (64, 32, fn.FN_LAYOUT_LINEAR, 32)
+    assert np.array_equal(fn.unpack_weights_w4(w4).cpu().numpy(), quantise(W.cpu(), None, 32, True))
+    w4.group = 64  # a smaller scale table, but another one
+    w4.K = 1 << 16
+    with pytest.raises(ValueError):
+        fn.unpack_weights_w4(w4)
+
+
+def test_fold_on_another_stream(fn):
+    W, g = torch.randn(520, 96, device=DEV), torch.rand(520, device=DEV) + 0.5
+    ref = fn.unpack_weights_w4(fn.fold_weights_w4(W, g, group=32, zero_points=True))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    w4 = fn.fold_weights_w4(W, g, group=32, zero_points=True, stream=side)
+    got = fn.unpack_weights_w4(w4, stream=side.cuda_stream)
+    side.synchronize()
+    assert torch.equal(got, ref)
