@@ -26,8 +26,9 @@
  *    a valid no-op.  Kernel launch failures return FN_ERR_HIP; faults during
  *    execution surface at the caller's next synchronisation.
  *  - Work is enqueued on `stream` (a hipStream_t; NULL = the default stream).
- *  - Results are deterministic: no atomics and no split reductions across
- *    workgroups, so repeated calls give bitwise-identical outputs.
+ *  - Results are deterministic: no atomics, and sums that are split across
+ *    workgroups (4-bit products, gradients) are joined in a fixed order, so
+ *    repeated calls give bitwise-identical outputs.
  *  - The packed weight layout written by fold_weights is opaque; only the
  *    library reads it.  One buffer serves both the many-row (matrix-core) and
  *    the few-row (bandwidth-bound) kernels.
@@ -456,7 +457,9 @@ size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout, 
  *           workspace serves calls that follow each other on a stream (FN_ERR_SIZE where it is
  *           too small, FN_ERR_NULL where it is needed and missing).
  * bias, inv_rms, outputs and errors as for the bf16-weight forms; no output may overlap an
- * input or another output (FN_ERR_ALIAS).  A row of a that holds a NaN or an infinity gives NaN. */
+ * input or another output (FN_ERR_ALIAS).  A row of a that holds a NaN or an infinity gives NaN.
+ * But for the sum of squares, no sum on the way overflows for |a|, |a g| up to 2^100 and |s| up to
+ * 2^80; beyond, a result that fp32 could hold may come out infinite or NaN. */
 int flashnorm_linear_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype,
                         const float* g, const void* W4, int64_t N, int group, float eps,
                         const float* bias, void* y, int64_t ldy, int y_dtype, float* inv_rms,

@@ -73,7 +73,9 @@ int run_w4(const W4Op& d) {
         (d.bias && overlaps(d.inv_rms, rbytes, d.bias, d.ncols * 4)))
       return FN_ERR_ALIAS;
   }
-  const int64_t NP = fn::packed_cols(N, d.glu), need = fn::w4_workspace(d.M, d.K, NP, d.glu, d.group, d.g != nullptr);
+  const int64_t NP = fn::packed_cols(N, d.glu), KB = fn::w4_blocks(d.K);
+  const fn::W4Plan plan = fn::w4_plan((int)d.M, (int)d.K, (int)KB, (int)NP, d.glu, d.group, d.g != nullptr);
+  const int64_t need = fn::w4_workspace(plan, d.M, KB, NP);
   if (need > 0) {
     if (!d.ws) return FN_ERR_NULL;
     if (!aligned16(d.ws)) return FN_ERR_ALIGN;
@@ -95,8 +97,8 @@ int run_w4(const W4Op& d) {
   ep.g_rt = d.g;
   fn::W4Args p{(const __bf16*)d.a, (int)d.M, (int)d.K, (int)d.lda, d.w4,
                fn::w4_scales(const_cast<void*>(d.w4), d.K, N, d.glu),
-               fn::w4_norms(const_cast<void*>(d.w4), d.K, N, d.glu, d.group), (int)NP, (int)fn::w4_blocks(d.K), d.group,
-               (int)d.ncols, (__bf16*)d.y, (int)d.ldy, d.epi, ep, d.ws, (hipStream_t)d.stream};
+               fn::w4_norms(const_cast<void*>(d.w4), d.K, N, d.glu, d.group), (int)NP, (int)KB, d.group,
+               (int)d.ncols, (__bf16*)d.y, (int)d.ldy, d.epi, ep, plan, d.ws, (hipStream_t)d.stream};
   const hipError_t e = fn::launch_w4(p);
   return e == hipErrorInvalidConfiguration ? FN_ERR_SIZE : status_of(e);
 }
@@ -159,9 +161,7 @@ int unpack_weights_w4(const void* W4, int64_t K, int64_t N, int layout, int grou
 size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout, int group) {
   if (M < 0 || M > kMaxRows || check_w4(K, N, layout, group)) return 0;
   const bool glu = layout == FN_LAYOUT_GLU;
-  const int64_t NP = fn::packed_cols(N, glu), plain = fn::w4_workspace(M, K, NP, glu, group, false);
-  const int64_t with_g = fn::w4_workspace(M, K, NP, glu, group, true);  // either call fits
-  return (size_t)(plain > with_g ? plain : with_g);
+  return (size_t)fn::w4_workspace(M, K, fn::packed_cols(N, glu), glu, group);
 }
 
 int flashnorm_linear_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype, const float* g, const void* W4,
@@ -172,13 +172,15 @@ int flashnorm_linear_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_
 }
 
 int flashnorm_glu_w4(const void* a, int64_t M, int64_t K, int64_t lda, int a_dtype, const float* g, const void* W4_gu,
-                     int64_t F, int group, float eps, void* out, int64_t ldo, int out_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+                     int64_t F, int group, float eps, void* out, int64_t ldo, int out_dtype, void* workspace,
+                     size_t workspace_bytes, void* stream) {
   return run_w4(W4Op{a, M, K, lda, a_dtype, g, W4_gu, F, 1, group, out, ldo, out_dtype, fn::EPI_GLU, eps, nullptr,
                      nullptr, nullptr, workspace, workspace_bytes, stream});
 }
 
 int rowscale_linear_w4(const void* x, int64_t M, int64_t K, int64_t ldx, int x_dtype, const void* W4, int64_t N,
-                       int group, const float* row_scale, void* y, int64_t ldy, int y_dtype, void* workspace, size_t workspace_bytes, void* stream) {
+                       int group, const float* row_scale, void* y, int64_t ldy, int y_dtype, void* workspace,
+                       size_t workspace_bytes, void* stream) {
   return run_w4(W4Op{x, M, K, ldx, x_dtype, nullptr, W4, N, 0, group, y, ldy, y_dtype, fn::EPI_ROWSCALE, 0.0f, nullptr,
                      nullptr, row_scale, workspace, workspace_bytes, stream});
 }

@@ -177,6 +177,15 @@ hipError_t launch_w4_pack(const uint8_t* codes, int64_t ldc, const float* scales
                           int64_t ldz, int64_t K, int64_t N, int glu, int group, void* w4, hipStream_t stream);
 hipError_t launch_w4_unpack(const void* w4, int64_t K, int64_t N, int glu, int group, float* out, int64_t ldo,
                             hipStream_t stream);
+// How a product goes: few rows or many, the workgroup shape, the splits of K and their k blocks.
+struct W4Plan {
+  bool many;
+  int shape, splits, kb_per_split;
+};
+W4Plan w4_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs);
+int64_t w4_workspace(const W4Plan& plan, int64_t M, int64_t KB, int64_t NP);  // bytes
+// The larger of a call's with a run-time g and without.
+int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu, int group);
 struct W4Args {
   const __bf16* a;
   int M, K, lda;
@@ -189,12 +198,12 @@ struct W4Args {
   int ldy;
   int epi;
   EpiArgs ep;  // ep.g_rt: run-time g, or nullptr
-  void* ws;    // w4_workspace bytes
+  W4Plan plan;
+  void* ws;  // w4_workspace bytes
   hipStream_t stream;
 };
 // hipErrorInvalidConfiguration: more workgroups than a launch takes.
 hipError_t launch_w4(const W4Args& p);
-int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu, int group, bool gs);
 
 // Block residual (residual.hip).
 struct ResidualArgs {

@@ -47,60 +47,83 @@ constexpr float kW4ManyUs = 7.15f, kW4ManyPerMK = 1.30f, kW4JoinUs = 2.99f, kW4J
 // The few-row kernel reads its rows once per column tile and is not looked at beyond this many.
 constexpr int kW4FewMaxM = 256;
 
+// A non-negative x rounded up (ceilf would be a call).
+static float up(float x) {
+  const float t = (float)(int64_t)x;
+  return t < x ? t + 1.0f : t;
+}
+
 static float shape_us(const W4Shape& s, int64_t wgs, int sets) {
-  const float r = (float)wgs / 256.0f, rounds = ceilf(r / s.per_cu);
-  const float in_last = ceilf(r - (rounds - 1.0f) * s.per_cu);
+  const float r = (float)wgs / 256.0f, rounds = up(r / s.per_cu);
+  const float in_last = up(r - (rounds - 1.0f) * s.per_cu);
   const float fill = s.per_cu > 1 ? (in_last - 1.0f) / (s.per_cu - 1) : 0.0f;
   return s.start * rounds + sets * (s.full * (rounds - 1.0f) + s.one + (s.full - s.one) * fill) + s.each * r;
 }
 
-struct W4Plan {
-  bool many;
-  int shape, splits, kb_per_split;
+// The least time of each kernel, and how (NP and KB: packed columns and k blocks).
+struct W4Best {
+  W4Plan plan;
+  float us;
 };
 
 // Smaller groups and a run-time g cost the few-row kernel most: a scale, a sum and four multiply-adds per group and
 // column, and two matrix-core operations for one.  Measured at 16..128 rows as factors of the shapes' times.
-W4Plan w4_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs) {
-  const float few_x = (group == 32 ? 1.55f : group == 64 ? 1.2f : 1.0f) * (gs ? 1.9f : 1.0f);
-  const float many_x = group == 32 ? 1.15f : group == 64 ? 1.04f : 1.0f;
-  W4Plan best{false, 0, 1, KB};
-  float best_us = 1e30f;
-  const float mk = (float)M * (float)K * 1e-6f;
-  if (M <= kW4FewMaxM) {
-    for (int i = 0; i < (glu ? kW4FewLinearOnly : (int)(sizeof(kW4Few) / sizeof(W4Shape))); ++i) {
-      const W4Shape& s = kW4Few[i];
-      if (i == kW4FewWide && (gs || M <= FN_W4_FEW_M)) continue;
-      const int64_t wgs = (int64_t)((M + 15) / 16) * ((NP + s.cols - 1) / s.cols);
-      const float us = kW4FewUs + kW4FewPerMK * mk + few_x * shape_us(s, wgs, (KB + s.ks - 1) / s.ks);
-      if (us < best_us) best_us = us, best = W4Plan{false, i, 1, KB};
-    }
-    if (M <= FN_W4_FEW_M) return best;
+static W4Best few_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs) {
+  W4Best best{{false, 0, 1, KB}, 1e30f};
+  if (M > kW4FewMaxM) return best;
+  const float x = (group == 32 ? 1.55f : group == 64 ? 1.2f : 1.0f) * (gs ? 1.9f : 1.0f);
+  for (int i = 0; i < (glu ? kW4FewLinearOnly : (int)(sizeof(kW4Few) / sizeof(W4Shape))); ++i) {
+    const W4Shape& s = kW4Few[i];
+    if (i == kW4FewWide && (gs || M <= FN_W4_FEW_M)) continue;
+    const int64_t wgs = (int64_t)((M + 15) / 16) * ((NP + s.cols - 1) / s.cols);
+    const float us = kW4FewUs + kW4FewPerMK * ((float)M * (float)K * 1e-6f) + x * shape_us(s, wgs, (KB + s.ks - 1) / s.ks);
+    if (us < best.us) best = W4Best{{false, i, 1, KB}, us};
   }
+  return best;
+}
+
+// Not looked for where no shape can take less than `bound`.
+static W4Best many_plan(int M, int K, int KB, int NP, int group, float bound) {
+  W4Best best{{true, 0, 1, KB}, 1e30f};
+  const float fixed = kW4ManyUs + kW4ManyPerMK * ((float)M * (float)K * 1e-6f);
+  if (fixed >= bound) return best;
+  const float x = group == 32 ? 1.15f : group == 64 ? 1.04f : 1.0f;
   for (int i = 0; i < (int)(sizeof(kW4Many) / sizeof(W4Shape)); ++i) {
     const W4Shape& s = kW4Many[i];
     const int64_t tiles = (int64_t)((M + s.rows - 1) / s.rows) * ((NP + s.cols - 1) / s.cols);
     for (int splits = 1; splits <= 16; splits *= 2) {
       if (splits > 1 && (tiles * splits > 1100 || KB < 2 * splits)) break;
       const int per = ((KB + splits - 1) / splits + s.ks - 1) / s.ks * s.ks, n = (KB + per - 1) / per;
-      float us = kW4ManyUs + kW4ManyPerMK * mk + many_x * shape_us(s, tiles * n, per / s.ks);
+      float us = fixed + x * shape_us(s, tiles * n, per / s.ks);
       if (n > 1) us += kW4JoinUs + kW4JoinPerMB * (float)n * (float)M * (float)NP * 4e-6f;
-      if (us < best_us) best_us = us, best = W4Plan{true, i, n, per};
+      if (us < best.us) best = W4Best{{true, i, n, per}, us};
     }
   }
   return best;
 }
 
+W4Plan w4_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs) {
+  const W4Best few = few_plan(M, K, KB, NP, glu, group, gs);
+  if (M <= FN_W4_FEW_M) return few.plan;
+  const W4Best many = many_plan(M, K, KB, NP, group, few.us);
+  return few.us <= many.us ? few.plan : many.plan;
+}
+
 // Workspace of a call: the rows' factors, the fp16 activations and the splits' sums; 0 for the few-row kernel.
 static int64_t factor_bytes(int64_t M) { return round_up(M * 4, 256); }
-static int64_t w4_ws(const W4Plan& plan, int64_t M, int64_t KB, int64_t NP) {
+int64_t w4_workspace(const W4Plan& plan, int64_t M, int64_t KB, int64_t NP) {
   if (!plan.many) return 0;
   return factor_bytes(M) + M * KB * (2 * kW4KB) + (plan.splits > 1 ? plan.splits * M * NP * 4 : 0);
 }
 
-int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu, int group, bool gs) {
+int64_t w4_workspace(int64_t M, int64_t K, int64_t NP, bool glu, int group) {
+  if (M <= FN_W4_FEW_M) return 0;
   const int KB = (int)w4_blocks(K);
-  return M > 0 ? w4_ws(w4_plan((int)M, (int)K, KB, (int)NP, glu, group, gs), M, KB, NP) : 0;
+  const float plain = few_plan((int)M, (int)K, KB, (int)NP, glu, group, false).us;
+  const float with_g = few_plan((int)M, (int)K, KB, (int)NP, glu, group, true).us;
+  const float slower = plain > with_g ? plain : with_g;
+  const W4Best many = many_plan((int)M, (int)K, KB, (int)NP, group, slower);
+  return slower <= many.us ? 0 : w4_workspace(many.plan, M, KB, NP);
 }
 
 template <bool NORM>
@@ -118,8 +141,7 @@ static hipError_t launch_w4_rows(const W4Args& p, _Float16* out, float* factor) 
 }
 
 hipError_t launch_w4(const W4Args& p) {
-  const bool glu = epi_is_glu(p.epi);
-  const W4Plan plan = w4_plan(p.M, p.K, p.KB, p.NP, glu, p.group, p.ep.g_rt != nullptr);
+  const W4Plan& plan = p.plan;
   const W4Shape& s = plan.many ? kW4Many[plan.shape] : kW4Few[plan.shape];
   const int64_t groups = (p.M + s.rows - 1) / s.rows, wgs = groups * ((p.NP + s.cols - 1) / s.cols) * plan.splits;
   // A launch has fewer than 2^32 threads: up to 1024 per workgroup, in the pass over the rows too.
