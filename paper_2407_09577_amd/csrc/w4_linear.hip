@@ -17,7 +17,7 @@ extern template hipError_t launch_w4_many<EPI_ROWSCALE>(const W4Gemm&, int, int,
 // `last` going from one to full as the last round fills up.  Beside it stand what the kernel's launches cost
 // (kW4FewUs, kW4ManyUs), the activations' pass and, with splits of K, the join of their sums.  The constants
 // are least-squares fits over 900 (few rows: 1..200 rows) and 500 (17..2048 rows) random shapes of K 256..11008
-// and 256..22016 columns, linear and GLU, groups of 128, each shape's weights read in turn from 400 MB: 6%
+// and 256..22016 columns, linear and GLU, groups of 128, each shape's weights read in turn from 400 MB: 5%
 // rms for the many-row shapes and 8 to 12% for the few-row ones, whose times are launches in large part.  The
 // shape so chosen took 0.8% (many rows) and 1.7% (few) more than the best of each call, in the mean.
 // One workgroup of four waves leaves a compute unit's SIMDs a wave each, which neither hides its reads nor its
@@ -34,16 +34,16 @@ static constexpr W4Shape kW4Few[] = {
     {16, 16, 8, 2, 0.901f, 0.942f, 0.437f, 0.0f},   {16, 16, 16, 1, 0.430f, 1.177f, 0.930f, 0.0f},
     {16, 48, 8, 2, 0.795f, 1.849f, 0.899f, 0.040f}};
 static constexpr W4Shape kW4Many[] = {
-    {128, 256, 1, 2, 3.834f, 3.102f, 1.939f, 1.011f}, {128, 128, 1, 2, 1.149f, 1.627f, 1.087f, 2.125f},
-    {96, 256, 1, 2, 2.860f, 2.324f, 1.520f, 1.548f},  {96, 128, 1, 3, 0.798f, 1.829f, 0.880f, 1.601f},
-    {64, 128, 2, 2, 0.327f, 1.964f, 1.165f, 1.769f},  {64, 128, 1, 4, 0.328f, 1.877f, 0.683f, 1.202f},
-    {32, 128, 2, 4, 0.0f, 2.856f, 0.857f, 1.097f},    {32, 64, 4, 2, 0.018f, 1.635f, 0.962f, 0.986f},
-    {96, 128, 2, 1, 0.946f, 1.464f, 1.368f, 2.698f},  {128, 128, 2, 1, 1.548f, 1.816f, 1.688f, 2.916f},
-    {32, 32, 8, 1, 0.051f, 1.638f, 1.187f, 1.483f}};
+    {128, 256, 1, 2, 3.165f, 3.130f, 1.989f, 1.234f}, {128, 128, 1, 2, 0.875f, 1.652f, 1.123f, 2.066f},
+    {96, 256, 1, 2, 2.034f, 2.360f, 1.570f, 1.851f},  {96, 128, 1, 3, 0.747f, 1.858f, 0.905f, 1.419f},
+    {64, 128, 2, 2, 0.282f, 1.972f, 1.184f, 1.612f},  {64, 128, 1, 4, 0.235f, 1.875f, 0.705f, 1.036f},
+    {32, 128, 2, 4, 0.0f, 2.838f, 0.858f, 1.003f},    {32, 64, 4, 2, 0.099f, 1.609f, 0.953f, 0.838f},
+    {96, 128, 2, 1, 0.910f, 1.486f, 1.410f, 2.521f},  {128, 128, 2, 1, 1.384f, 1.805f, 1.742f, 2.935f},
+    {32, 32, 8, 1, 0.217f, 1.577f, 1.160f, 1.203f}};
 constexpr int kW4FewWide = 3;        // several row groups without a run-time g: elsewhere never the least time
 constexpr int kW4FewLinearOnly = 6;  // from here on: an odd number of column blocks holds no gate/up pairs
 constexpr float kW4FewUs = 3.89f, kW4FewPerMK = 1.01f;
-constexpr float kW4ManyUs = 7.15f, kW4ManyPerMK = 1.30f, kW4JoinUs = 2.99f, kW4JoinPerMB = 0.223f;
+constexpr float kW4ManyUs = 7.14f, kW4ManyPerMK = 0.859f, kW4JoinUs = 3.04f, kW4JoinPerMB = 0.255f;
 // The few-row kernel reads its rows once per column tile and is not looked at beyond this many.
 constexpr int kW4FewMaxM = 256;
 

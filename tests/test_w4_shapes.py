@@ -36,16 +36,16 @@ FEW = [  # read straight from memory, then staged through LDS (kW4StagedM rows a
     (5, (2, 144, 4307), (1, 152, 40)), (5, (6, 144, 4199), (13, 152, 40)), (6, (1, 144, 41), None), (6, (6, 144, 41), None),
     (7, (1, 1056, 41), None), (7, (11, 1048, 41), None), (8, (1, 520, 8809), None), (8, (6, 520, 8225), None)]
 MANY = [  # in one pass, then with K split
-    (0, (582, 144, 18777), (769, 144, 14346)), (0, (106, 9464, 8414), (101, 9312, 8436)),
-    (1, (329, 144, 17885), (321, 152, 16834)), (1, (102, 8240, 4819), (114, 4392, 8358)),
-    (2, (388, 144, 20475), (388, 144, 20404)), (2, (65, 8280, 8539), (65, 7240, 8574)),
-    (3, (81, 144, 21709), (84, 144, 20822)), (3, (1401, 8720, 65), (803, 10248, 138)),
-    (4, (803, 408, 1160), (300, 400, 3252)), (4, (717, 6232, 66), (685, 6320, 68)),
-    (5, (1430, 144, 658), (830, 144, 1164)), (5, (417, 6360, 130), (723, 9328, 68)),
-    (6, (262, 152, 40), (286, 144, 40)), (6, (370, 5304, 65), (356, 5144, 66)),
+    (0, (582, 144, 18777), (769, 144, 14346)), (0, (106, 6152, 16642), (102, 10872, 8336)),
+    (1, (323, 264, 18241), (324, 264, 17480)), (1, (102, 8240, 4819), (99, 5352, 8314)),
+    (2, (388, 144, 20475), (388, 144, 20404)), (2, (65, 8280, 8539), (70, 8280, 8766)),
+    (3, (81, 144, 21709), (269, 144, 7152)), (3, (1357, 9360, 67), (803, 10248, 138)),
+    (4, (329, 392, 3022), (547, 392, 1830)), (4, (717, 6232, 66), (685, 6320, 68)),
+    (5, (1430, 144, 658), (830, 144, 1164)), (5, (417, 6360, 130), (802, 9312, 66)),
+    (6, (262, 152, 40), (286, 144, 40)), (6, (370, 5304, 65), (452, 4112, 72)),
     (7, (269, 264, 41), (258, 264, 42)), (7, (262, 3104, 42), (261, 3120, 42)),
-    (8, (65, 1056, 16867), (130, 648, 13058)), (8, (1163, 10456, 65), (1134, 10824, 70)),
-    (9, (99, 904, 18987), (98, 928, 19618)), (9, (114, 4120, 4671), (113, 4152, 4716)),
+    (8, (129, 664, 13672), (130, 648, 13058)), (8, (1163, 10456, 65), (1384, 10696, 66)),
+    (9, (98, 1160, 16417), (97, 1208, 16724)), (9, (1357, 6296, 331), (97, 5720, 5636)),
     (10, (283, 520, 40), (262, 536, 42)), (10, (264, 9240, 40), (17, 10344, 44))]
 CALLS = [(False, i % 2 == 1, s, c, glu) for i, (s, *cs) in enumerate(FEW) for glu, c in enumerate(cs) if c] + \
         [(True, i % 2 == 1, s, c, glu) for i, (s, *cs) in enumerate(MANY) for glu, c in enumerate(cs) if c]
