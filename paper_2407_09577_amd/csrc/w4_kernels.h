@@ -368,7 +368,8 @@ struct W4Gemm {
   const float* bias;
   __bf16* y;
   int ldy;
-  int groups, splits, kb_per_split;
+  int groups, panel;  // row groups, and how many of them go through the column tiles together
+  int splits, kb_per_split;
   float* partial;  // [splits][M][NP]
 };
 
@@ -386,13 +387,10 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
 
   const int q8 = gridDim.x / kXcds, r8 = gridDim.x % kXcds, x8 = blockIdx.x % kXcds;
   int logical = x8 * q8 + min(x8, r8) + blockIdx.x / kXcds;
-  // Row groups in pairs, column tiles within a pair: an XCD's workgroups share two groups' activations (twice the
-  // bytes of the codes) in its L2, where all the groups' had to come again for every few tiles (2048 x 11008 -> 4096:
-  // 187 us with the groups innermost, 177 so, and no different in panels of four and eight).
-  const int tiles = (p.NP / 16 + CB - 1) / CB, pair = logical / (2 * tiles * p.splits);
-  logical -= pair * (2 * tiles * p.splits);
-  const int in_pair = min(2, p.groups - 2 * pair), grp = 2 * pair + logical % in_pair;
-  logical /= in_pair;
+  const int tiles = (p.NP / 16 + CB - 1) / CB, panel = logical / (p.panel * tiles * p.splits);
+  logical -= panel * (p.panel * tiles * p.splits);
+  const int in_panel = min(p.panel, p.groups - panel * p.panel), grp = panel * p.panel + logical % in_panel;
+  logical /= in_panel;
   const int split = logical % p.splits, tile = logical / p.splits;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
