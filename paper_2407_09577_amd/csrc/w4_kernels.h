@@ -37,14 +37,14 @@ __device__ __forceinline__ void split_ag(const bf16x8& a, const f32x4& g0, const
   }
 }
 
-// Few rows: bound by the weight stream.  A workgroup owns 16 rows and NCB column blocks; its KS waves take sets
-// of U code blocks (128 k each) in turn, the next set's loads in flight while the present one is multiplied, and
+// Few rows: bound by the weight stream.  A workgroup owns RG blocks of 16 rows and NCB column blocks; its KS waves
+// take code blocks (128 k each) in turn, the next one's loads in flight while the present one is multiplied, and
 // the partial products meet in LDS in a fixed order.
 // A wave's activations come straight in the matrix-core order, where sixteen rows lie in one load, or STAGED: read
 // along the rows and turned in a slot of LDS of its own.  That halves the requests of a load of sixteen rows
 // (4096 -> 6144 with one column block a wave: 11.9 -> 9.1 us) and only adds a wait to one of a row or two
 // (two blocks: 6.6 -> 7.6).
-template <int NCB, int KS, int U, int GB, int EPI, bool GS, bool STAGED>
+template <int NCB, int KS, int RG, int GB, int EPI, bool GS, bool STAGED>
 __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restrict__ a, int M, int K, int lda,
                                                          const void* __restrict__ codes,
                                                          const unsigned* __restrict__ scales, int NP, int KB, int ncols,
@@ -53,17 +53,17 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
   constexpr int NG = 4 / GB, STEP = epi_is_glu(EPI) ? 2 : 1;
   static_assert(NCB % STEP == 0, "GLU needs gate/up block pairs");
   // Each wave's slot for a block's activations, then (behind a barrier) the partial products.
-  static_assert(STAGED || !GS, "a g is split on its way through LDS");
-  constexpr int PLANES = GS ? 2 : 1, SLOT = STAGED ? 256 * PLANES : 0;  // units of a wave's slot
-  constexpr int UNITS = KS * (SLOT > 64 * NCB ? SLOT : 64 * NCB);
+  static_assert(STAGED || (!GS && RG == 1), "a g is split on its way through LDS, and 32 rows are turned there");
+  constexpr int PLANES = GS ? 2 : 1, SLOT = STAGED ? 256 * PLANES * RG : 0;  // units of a wave's slot
+  constexpr int UNITS = KS * (SLOT > 64 * NCB * RG ? SLOT : 64 * NCB * RG);
   __shared__ u32x4 smem[UNITS];
-  __shared__ float red_ss[KS][16];
+  __shared__ float red_ss[KS][16 * RG];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   // The row groups of a column tile are neighbours on one XCD and share its codes in that L2.
   const int q8 = gridDim.x / kXcds, r8 = gridDim.x % kXcds, x8 = blockIdx.x % kXcds;
   const int logical = x8 * q8 + min(x8, r8) + blockIdx.x / kXcds;
-  const int tile = logical / groups, m0 = logical % groups * 16, rows = min(16, M - m0);
+  const int tile = logical / groups, m0 = logical % groups * (16 * RG), rows = min(16 * RG, M - m0);
   const int cb0 = tile * NCB, npb = NP / 16;
   const int lrow = lane & 15, lch = lane >> 4;
   const __amdgpu_buffer_rsrc_t rs_a =
@@ -77,35 +77,33 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
   const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{one2, one2, one2, one2});
 
   struct Set {
-    u32x4 w[U][NCB], a[U][4], g[U][GS ? 2 : 1];
-    unsigned s[U][NG][NCB];
+    u32x4 w[NCB], a[RG][4], g[GS ? 2 : 1];
+    unsigned s[NG][NCB];
   };
-  auto load_set = [&](int kb0, Set& t) __attribute__((always_inline)) {
+  auto load_set = [&](int kb, Set& t) __attribute__((always_inline)) {
+    const bool ok = kb < KB;
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      const int kb = kb0 + i * KS;
-      const bool ok = kb < KB;
+    for (int c = 0; c < NCB; ++c)
+      t.w[c] = load_buf16<kCachePolicyNT>(rs_w, ok ? (unsigned)(kb * npb + cb0 + c) * 1024u + lane * 16 : kOobOffset);
+#pragma unroll
+    for (int j = 0; j < NG; ++j)
 #pragma unroll
       for (int c = 0; c < NCB; ++c)
-        t.w[i][c] = load_buf16<kCachePolicyNT>(rs_w, ok ? (unsigned)(kb * npb + cb0 + c) * 1024u + lane * 16 : kOobOffset);
+        t.s[j][c] = __builtin_amdgcn_raw_buffer_load_b32(
+            rs_s, ok ? (unsigned)((kb * NG + j) * NP + (cb0 + c) * 16 + lrow) * 4u : kOobOffset, 0, 0);
 #pragma unroll
-      for (int j = 0; j < NG; ++j)
-#pragma unroll
-        for (int c = 0; c < NCB; ++c)
-          t.s[i][j][c] = __builtin_amdgcn_raw_buffer_load_b32(
-              rs_s, ok ? (unsigned)((kb * NG + j) * NP + (cb0 + c) * 16 + lrow) * 4u : kOobOffset, 0, 0);
+    for (int q = 0; q < RG; ++q)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         // Staged: sixteen lanes read one row's 256 bytes, four rows at a time.  Else: the matrix-core order.
-        const int row = STAGED ? 4 * j + lch : lrow, k = kb * kW4KB + (STAGED ? 8 * lrow : 32 * j + 8 * lch);
+        const int row = 16 * q + (STAGED ? 4 * j + lch : lrow), k = kb * kW4KB + (STAGED ? 8 * lrow : 32 * j + 8 * lch);
         if (GS && 4 * j >= rows) continue;  // what a row costs is its splitting (else the branch costs more)
-        t.a[i][j] = load_buf16(rs_a, row < rows && k < K ? (unsigned)(row * lda + k) * 2 : kOobOffset);
+        t.a[q][j] = load_buf16(rs_a, row < rows && k < K ? (unsigned)(row * lda + k) * 2 : kOobOffset);
       }
-      if constexpr (GS) {  // this lane's eight k, the same for its four rows; past K: zeros
-        const unsigned k = (unsigned)(kb * kW4KB + 8 * lrow);
-        t.g[i][0] = load_buf16(rs_g, k * 4);
-        t.g[i][1] = load_buf16(rs_g, k * 4 + 16);
-      }
+    if constexpr (GS) {  // this lane's eight k, the same for its four rows; past K: zeros
+      const unsigned k = (unsigned)(kb * kW4KB + 8 * lrow);
+      t.g[0] = load_buf16(rs_g, k * 4);
+      t.g[1] = load_buf16(rs_g, k * 4 + 16);
     }
   };
   // Piece (k block u, chunk c) of row r in the slot: where the matrix-core order reads it, at a position XORed
@@ -118,70 +116,82 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
       for (int i = 0; i < SLOT / 64; ++i) own[i * 64 + lane] = u32x4{0, 0, 0, 0};
     }
   }
-  f32x4 acc[NCB];
+  f32x4 acc[RG][NCB];
+  float ss[RG], ss4[4] = {0.f, 0.f, 0.f, 0.f};  // ss4, with g: of the raw rows 4 j + lch
 #pragma unroll
-  for (int c = 0; c < NCB; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float ss = 0.f, ss4[4] = {0.f, 0.f, 0.f, 0.f};  // GS: of the raw rows 4 j + lch
+  for (int q = 0; q < RG; ++q) {
+    ss[q] = 0.f;
+#pragma unroll
+    for (int c = 0; c < NCB; ++c) acc[q][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   auto compute_set = [&](const Set& t) __attribute__((always_inline)) {
+    if constexpr (STAGED) {
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-      if constexpr (STAGED) {
+      for (int q = 0; q < RG; ++q)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           if (GS && 4 * j >= rows) continue;  // the slot holds zeros there
           const int at = slot(lrow >> 2, 4 * j + lch, lrow & 3);
           if constexpr (GS) {
             bf16x8 hi, lo;
-            if constexpr (kSS) ss4[j] = sumsq8(__builtin_bit_cast(bf16x8, t.a[i][j]), ss4[j]);
-            split_ag(__builtin_bit_cast(bf16x8, t.a[i][j]), __builtin_bit_cast(f32x4, t.g[i][0]),
-                     __builtin_bit_cast(f32x4, t.g[i][1]), hi, lo);
+            if constexpr (kSS) ss4[j] = sumsq8(__builtin_bit_cast(bf16x8, t.a[q][j]), ss4[j]);
+            split_ag(__builtin_bit_cast(bf16x8, t.a[q][j]), __builtin_bit_cast(f32x4, t.g[0]),
+                     __builtin_bit_cast(f32x4, t.g[1]), hi, lo);
             own[at] = __builtin_bit_cast(u32x4, hi);
             own[256 + at] = __builtin_bit_cast(u32x4, lo);
           } else {
-            own[at] = t.a[i][j];
+            own[256 * q + at] = t.a[q][j];
           }
         }
-      }
+    }
 #pragma unroll
-      for (int j = 0; j < NG; ++j) {
-        bf16x8 av[GB], al[GB];
-        f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};  // the group's sum of each row's activations
+    for (int j = 0; j < NG; ++j) {
+      bf16x8 av[RG][GB], al[GB];
+      f32x4 sum[RG];  // the group's sum of each row's activations
+#pragma unroll
+      for (int q = 0; q < RG; ++q) {
+        sum[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int b = 0; b < GB; ++b) {
           const int u = j * GB + b;
-          av[b] = __builtin_bit_cast(bf16x8, STAGED ? own[slot(u, lrow, lch)] : t.a[i][u]);
-          if constexpr (kSS && !GS) ss = sumsq8(av[b], ss);
+          av[q][b] = __builtin_bit_cast(bf16x8, STAGED ? own[256 * q + slot(u, lrow, lch)] : t.a[q][u]);
+          if constexpr (kSS && !GS) ss[q] = sumsq8(av[q][b], ss[q]);
           if constexpr (GS) {
             al[b] = __builtin_bit_cast(bf16x8, own[256 + slot(u, lrow, lch)]);
-            sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al[b], ones, sum, 0, 0, 0);
+            sum[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al[b], ones, sum[q], 0, 0, 0);
           }
-          sum = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[b], ones, sum, 0, 0, 0);
+          sum[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[q][b], ones, sum[q], 0, 0, 0);
         }
+      }
 #pragma unroll
-        for (int c = 0; c < NCB; ++c) {
-          f32x4 part = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int c = 0; c < NCB; ++c) {
+        f32x4 part[RG];
 #pragma unroll
-          for (int b = 0; b < GB; ++b) {
-            const bf16x8 wv = w4_widen(t.w[i][c][j * GB + b]);
-            if constexpr (GS) part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al[b], wv, part, 0, 0, 0);
-            part = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[b], wv, part, 0, 0, 0);
-          }
-          const float s = w4_scale(t.s[i][j][c]), bias = -kW4Bias - w4_zero(t.s[i][j][c]);
+        for (int q = 0; q < RG; ++q) part[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int r = 0; r < 4; ++r) acc[c][r] = fmaf(s, fmaf(bias, sum[r], part[r]), acc[c][r]);
+        for (int b = 0; b < GB; ++b) {
+          const bf16x8 wv = w4_widen(t.w[c][j * GB + b]);
+          if constexpr (GS) part[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al[b], wv, part[0], 0, 0, 0);
+#pragma unroll
+          for (int q = 0; q < RG; ++q) part[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[q][b], wv, part[q], 0, 0, 0);
         }
+        const float s = w4_scale(t.s[j][c]), bias = -kW4Bias - w4_zero(t.s[j][c]);
+#pragma unroll
+        for (int q = 0; q < RG; ++q)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) acc[q][c][r] = fmaf(s, fmaf(bias, sum[q][r], part[q][r]), acc[q][c][r]);
       }
     }
   };
   Set t0, t1;
   load_set(wave, t0);
-  for (int kb0 = wave; kb0 < KB; kb0 += 2 * U * KS) {
-    load_set(kb0 + U * KS, t1);
+  for (int kb = wave; kb < KB; kb += 2 * KS) {
+    load_set(kb + KS, t1);
     __builtin_amdgcn_sched_barrier(0);
     compute_set(t0);
     __builtin_amdgcn_sched_barrier(0);
-    if (kb0 + U * KS >= KB) break;
-    load_set(kb0 + 2 * U * KS, t0);
+    if (kb + KS >= KB) break;
+    load_set(kb + 2 * KS, t0);
     __builtin_amdgcn_sched_barrier(0);
     compute_set(t1);
     __builtin_amdgcn_sched_barrier(0);
@@ -195,32 +205,39 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
       if (lrow == 0) red_ss[wave][4 * j + lch] = ss4[j];
     }
   } else if constexpr (kSS) {
-    ss += __shfl_xor(ss, 16);
-    ss += __shfl_xor(ss, 32);
-    if (lane < 16) red_ss[wave][lane] = ss;
+#pragma unroll
+    for (int q = 0; q < RG; ++q) {
+      ss[q] += __shfl_xor(ss[q], 16);
+      ss[q] += __shfl_xor(ss[q], 32);
+      if (lane < 16) red_ss[wave][16 * q + lane] = ss[q];
+    }
   }
   __syncthreads();
   f32x4* red = reinterpret_cast<f32x4*>(smem);
 #pragma unroll
-  for (int c = 0; c < NCB; ++c) red[(wave * NCB + c) * 64 + lane] = acc[c];
-  __syncthreads();
-  for (int o = wave; o < NCB / STEP; o += KS) {
-    f32x4 v = red[o * STEP * 64 + lane], u = red[(o * STEP + STEP - 1) * 64 + lane];
+  for (int q = 0; q < RG; ++q)
 #pragma unroll
-    for (int w = 1; w < KS; ++w) {
-      v += red[(w * NCB + o * STEP) * 64 + lane];
-      if constexpr (STEP == 2) u += red[(w * NCB + o * STEP + 1) * 64 + lane];
+    for (int c = 0; c < NCB; ++c) red[((wave * RG + q) * NCB + c) * 64 + lane] = acc[q][c];
+  __syncthreads();
+  constexpr int OUTS = NCB / STEP;  // output column blocks
+  for (int i = wave; i < RG * OUTS; i += KS) {
+    const int q = i / OUTS, o = i % OUTS;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f}, u = v;
+#pragma unroll
+    for (int w = 0; w < KS; ++w) {
+      v += red[((w * RG + q) * NCB + o * STEP) * 64 + lane];
+      if constexpr (STEP == 2) u += red[((w * RG + q) * NCB + o * STEP + 1) * 64 + lane];
     }
     const int n = (cb0 / STEP + o) * 16 + lrow;
     const float bias = EPI == EPI_RMS && ep.bias && n < ncols ? ep.bias[n] : 0.0f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      if (4 * lch + r >= rows) break;
-      const int m = m0 + 4 * lch + r;
+      const int row = 16 * q + 4 * lch + r, m = m0 + row;
+      if (row >= rows) break;
       float ss_t = 0.f;
       if constexpr (kSS) {
 #pragma unroll
-        for (int w = 0; w < KS; ++w) ss_t += red_ss[w][4 * lch + r];
+        for (int w = 0; w < KS; ++w) ss_t += red_ss[w][row];
       }
       const float s = w4_row_scale<EPI>(ss_t, ep, m);
       if constexpr (epi_exports_s(EPI)) {
@@ -639,37 +656,38 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Gemm p) {
 // Rows from which the activations are staged: at 5 x 11008 -> 4096 the two are within 4% of each other.
 constexpr int kW4StagedM = 6;
 
-template <int NCB, int KS, int GB, int EPI, bool GS>
+template <int NCB, int KS, int RG, int GB, int EPI, bool GS>
 static hipError_t launch_w4_few_cfg(const W4Args& p) {
-  const int tiles = (p.NP / 16 + NCB - 1) / NCB, groups = (p.M + 15) / 16;
+  const int tiles = (p.NP / 16 + NCB - 1) / NCB, groups = (p.M + 16 * RG - 1) / (16 * RG);
   auto go = [&](auto kernel) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)tiles * groups), dim3(64 * KS), 0, p.stream, p.a, p.M, p.K, p.lda, p.codes,
                        p.scales, p.NP, p.KB, p.ncols, p.y, p.ldy, p.ep, groups);
     return hipGetLastError();
   };
-  if constexpr (!GS && NCB < 8)
-    if (p.M < kW4StagedM) return go(w4_few_kernel<NCB, KS, 1, GB, EPI, GS, false>);
-  return go(w4_few_kernel<NCB, KS, 1, GB, EPI, GS, true>);
+  if constexpr (!GS && RG == 1)
+    if (p.M < kW4StagedM) return go(w4_few_kernel<NCB, KS, RG, GB, EPI, GS, false>);
+  return go(w4_few_kernel<NCB, KS, RG, GB, EPI, GS, true>);
 }
 
 // The shapes of w4_linear.hip's kW4Few, in its order.
 template <int GB, int EPI, bool GS>
 static hipError_t launch_w4_few_g(const W4Args& p, int shape) {
   switch (shape) {
-    case 0: return launch_w4_few_cfg<2, 8, GB, EPI, GS>(p);
-    case 1: return launch_w4_few_cfg<4, 8, GB, EPI, GS>(p);
-    case 2: return launch_w4_few_cfg<6, 8, GB, EPI, GS>(p);
-    case 3:
-      if constexpr (!GS) return launch_w4_few_cfg<8, 8, GB, EPI, GS>(p);
-      break;
-    case 4: return launch_w4_few_cfg<4, 4, GB, EPI, GS>(p);
-    case 5: return launch_w4_few_cfg<2, 4, GB, EPI, GS>(p);
-    default:
-      if constexpr (!epi_is_glu(EPI)) {
-        if (shape == 6) return launch_w4_few_cfg<1, 8, GB, EPI, GS>(p);
-        if (shape == 7) return launch_w4_few_cfg<1, 16, GB, EPI, GS>(p);
-        if (shape == 8) return launch_w4_few_cfg<3, 8, GB, EPI, GS>(p);
-      }
+    case 0: return launch_w4_few_cfg<2, 8, 1, GB, EPI, GS>(p);
+    case 1: return launch_w4_few_cfg<4, 8, 1, GB, EPI, GS>(p);
+    case 2: return launch_w4_few_cfg<6, 8, 1, GB, EPI, GS>(p);
+    case 3: return launch_w4_few_cfg<4, 4, 1, GB, EPI, GS>(p);
+    case 4: return launch_w4_few_cfg<2, 4, 1, GB, EPI, GS>(p);
+  }
+  if constexpr (!GS) {
+    if (shape == 5) return launch_w4_few_cfg<4, 8, 2, GB, EPI, GS>(p);
+    if constexpr (GB == 4)
+      if (shape == 6) return launch_w4_few_cfg<6, 8, 2, GB, EPI, GS>(p);
+  }
+  if constexpr (!epi_is_glu(EPI)) {
+    if (shape == 7) return launch_w4_few_cfg<1, 8, 1, GB, EPI, GS>(p);
+    if (shape == 8) return launch_w4_few_cfg<1, 16, 1, GB, EPI, GS>(p);
+    if (shape == 9) return launch_w4_few_cfg<3, 8, 1, GB, EPI, GS>(p);
   }
   return hipErrorInvalidValue;
 }

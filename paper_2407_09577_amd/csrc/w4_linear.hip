@@ -16,23 +16,24 @@ extern template hipError_t launch_w4_many<EPI_ROWSCALE>(const W4Gemm&, int, int,
 //   start ceil(r / per_cu) + sets (full (ceil(r / per_cu) - 1) + last) + each r,
 // `last` going from one to full as the last round fills up.  Beside it stand what the kernel's launches cost
 // (kW4FewUs, kW4ManyUs), the activations' pass and, with splits of K, the join of their sums.  The constants
-// are least-squares fits over 900 (few rows: 1..200 rows) and 500 (17..2048 rows) random shapes of K 256..11008
+// are least-squares fits over 900 (few rows: 1..256 rows) and 500 (17..2048 rows) random shapes of K 256..11008
 // and 256..22016 columns, linear and GLU, groups of 128, each shape's weights read in turn from 400 MB: 5%
 // rms for the many-row shapes and 8 to 12% for the few-row ones, whose times are launches in large part.  The
-// shape so chosen took 0.8% (many rows) and 1.7% (few) more than the best of each call, in the mean.
+// shape so chosen took 0.8% (many rows) and 1.7 to 2.8% (few) more than the best of each call, in the mean.
 // One workgroup of four waves leaves a compute unit's SIMDs a wave each, which neither hides its reads nor its
 // widening: where a call has no more than a workgroup for each, two or eight k groups do (695 x 3928 x 3520:
-// 42.4 us with 96 x 128 tiles, 35.2 with two k groups on each).
+// 42.4 us with 96 x 128 tiles, 35.2 with two k groups on each).  Two blocks of rows on a few-row workgroup widen the
+// codes once for both, where the width alone fills the chip (32 x 4096 -> 22016 GLU: 21.5 us with one, 18.6 with two).
 struct W4Shape {
   int rows, cols, ks, per_cu;
   float start, full, one, each;
 };
 static constexpr W4Shape kW4Few[] = {
-    {16, 32, 8, 2, 0.894f, 1.359f, 0.642f, 0.0f},   {16, 64, 8, 2, 0.510f, 2.930f, 1.183f, 0.431f},
-    {16, 96, 8, 2, 0.098f, 4.176f, 1.694f, 1.151f}, {16, 128, 8, 1, 0.0f, 2.924f, 2.265f, 1.162f},
-    {16, 64, 4, 4, 0.376f, 2.450f, 1.010f, 0.195f}, {16, 32, 4, 4, 0.734f, 1.431f, 0.644f, 0.0f},
-    {16, 16, 8, 2, 0.901f, 0.942f, 0.437f, 0.0f},   {16, 16, 16, 1, 0.430f, 1.177f, 0.930f, 0.0f},
-    {16, 48, 8, 2, 0.795f, 1.849f, 0.899f, 0.040f}};
+    {16, 32, 8, 2, 0.586f, 1.376f, 0.630f, 0.0f},   {16, 64, 8, 2, 0.390f, 2.886f, 1.144f, 0.315f},
+    {16, 96, 8, 2, 0.083f, 4.234f, 1.640f, 0.719f}, {16, 64, 4, 4, 0.522f, 2.440f, 0.829f, 0.137f},
+    {16, 32, 4, 4, 0.781f, 1.411f, 0.502f, 0.0f},   {32, 64, 8, 1, 0.0f, 2.426f, 1.812f, 0.912f},
+    {32, 96, 8, 1, 0.244f, 3.002f, 2.480f, 1.539f}, {16, 16, 8, 2, 0.817f, 0.751f, 0.411f, 0.0f},
+    {16, 16, 16, 1, 0.502f, 0.684f, 0.890f, 0.0f},  {16, 48, 8, 2, 0.733f, 1.826f, 0.826f, 0.0f}};
 static constexpr W4Shape kW4Many[] = {
     {128, 256, 1, 2, 3.165f, 3.130f, 1.989f, 1.234f}, {128, 128, 1, 2, 0.875f, 1.652f, 1.123f, 2.066f},
     {96, 256, 1, 2, 2.034f, 2.360f, 1.570f, 1.851f},  {96, 128, 1, 3, 0.747f, 1.858f, 0.905f, 1.419f},
@@ -40,9 +41,8 @@ static constexpr W4Shape kW4Many[] = {
     {32, 128, 2, 4, 0.0f, 2.838f, 0.858f, 1.003f},    {32, 64, 4, 2, 0.099f, 1.609f, 0.953f, 0.838f},
     {96, 128, 2, 1, 0.910f, 1.486f, 1.410f, 2.521f},  {128, 128, 2, 1, 1.384f, 1.805f, 1.742f, 2.935f},
     {32, 32, 8, 1, 0.217f, 1.577f, 1.160f, 1.203f}};
-constexpr int kW4FewWide = 3;        // several row groups without a run-time g: elsewhere never the least time
-constexpr int kW4FewLinearOnly = 6;  // from here on: an odd number of column blocks holds no gate/up pairs
-constexpr float kW4FewUs = 3.89f, kW4FewPerMK = 1.01f;
+constexpr int kW4FewLinearOnly = 7;  // from here on: an odd number of column blocks holds no gate/up pairs
+constexpr float kW4FewUs = 4.15f, kW4FewPerMK = 0.915f;
 constexpr float kW4ManyUs = 7.14f, kW4ManyPerMK = 0.859f, kW4JoinUs = 3.04f, kW4JoinPerMB = 0.255f;
 // The few-row kernel reads its rows once per column tile and is not looked at beyond this many.
 constexpr int kW4FewMaxM = 256;
@@ -74,8 +74,9 @@ static W4Best few_plan(int M, int K, int KB, int NP, bool glu, int group, bool g
   const float x = (group == 32 ? 1.55f : group == 64 ? 1.2f : 1.0f) * (gs ? 1.9f : 1.0f);
   for (int i = 0; i < (glu ? kW4FewLinearOnly : (int)(sizeof(kW4Few) / sizeof(W4Shape))); ++i) {
     const W4Shape& s = kW4Few[i];
-    if (i == kW4FewWide && (gs || M <= FN_W4_FEW_M)) continue;
-    const int64_t wgs = (int64_t)((M + 15) / 16) * ((NP + s.cols - 1) / s.cols);
+    // Beside two blocks of rows there are no registers for a g's halves, nor for six columns' scales of small groups.
+    if (s.rows == 32 && (M <= 16 || gs || (s.cols == 96 && group < 128))) continue;
+    const int64_t wgs = (int64_t)((M + s.rows - 1) / s.rows) * ((NP + s.cols - 1) / s.cols);
     const float us = kW4FewUs + kW4FewPerMK * ((float)M * (float)K * 1e-6f) + x * shape_us(s, wgs, (KB + s.ks - 1) / s.ks);
     if (us < best.us) best = W4Best{{false, i, 1, KB}, us};
   }
