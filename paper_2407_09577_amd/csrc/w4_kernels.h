@@ -44,6 +44,9 @@ __device__ __forceinline__ void split_ag(const bf16x8& a, const f32x4& g0, const
 // along the rows and turned in a slot of LDS of its own.  That halves the requests of a load of sixteen rows
 // (4096 -> 6144 with one column block a wave: 11.9 -> 9.1 us) and only adds a wait to one of a row or two
 // (two blocks: 6.6 -> 7.6).
+// Kernel times: 1 x 4096 -> 6144 6.9 us, 16 x 4096 -> 22016 GLU 14.5 us for 50 MB, beside 3.1 us of a kernel that does
+// nothing: the stream itself runs at 3.5 to 4.4 TB/s.  64 x 11008 -> 4096 (18.6 us a call) is bound by the widening,
+// once for each 16 rows, and its waits; the matrix cores are busy for 11% of it.
 template <int NCB, int KS, int RG, int GB, int EPI, bool GS, bool STAGED>
 __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restrict__ a, int M, int K, int lda,
                                                          const void* __restrict__ codes,
@@ -259,7 +262,8 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
 // One workgroup per row: the row's squares and largest value, then its fp16 form, [KB * 128] with zeros
 // past K, and the factor that the outputs take: (1 / RMSe, or the given row scale) / the power of two.
 // With g the values are a g, rounded to fp16.  A row that holds a NaN or an infinity gets a NaN factor.
-// T threads hold up to H pieces of 16 bytes each; H = 0: the row is read twice.
+// T threads hold up to H pieces of 16 bytes each; H = 0: the row is read twice.  Bound by its launch and one trip to
+// memory: 333 x 4096 5.2 us.
 template <bool NORM, int T, int H>
 __global__ __launch_bounds__(T) void w4_rows_kernel(const __bf16* __restrict__ a, int K, int lda,
                                                     const float* __restrict__ g, const float* __restrict__ row_scale,
@@ -374,6 +378,10 @@ __device__ __forceinline__ f16x8 w4_widen_f16(unsigned w, f16x2 zero, f16x2 zero
 // ring of NST stages, NST - 1 sets ahead: 16 lanes bring one row's 256 bytes, 16-byte piece j of row r at
 // position j ^ (r % 16), so that the sixteen rows of an operand read lie in different banks.
 // With several `splits` of K each workgroup writes its fp32 sums and w4_join_kernel finishes them.
+// Bound by the matrix cores where there are enough workgroups, else by the waits in one set: 2048 x 4096 -> 22016 GLU
+// 321 us, 1.15 PFLOP/s with the matrix cores busy for half of the time; a set of 128 k takes a workgroup that is alone
+// on its compute unit 2600 cycles, 1024 of them matrix-core operations.  Weights through LDS as well, a third stage,
+// operands read six or eight steps ahead and widening spread over the steps, into the next set's first, did not help.
 struct W4Gemm {
   const _Float16* a;  // [M][KP]
   int M, KP;
@@ -618,7 +626,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
 }
 
 // Joins the splits of K in order and applies the epilogue: one thread per four packed columns of a row (GLU:
-// four gate columns and their up columns).
+// four gate columns and their up columns).  Bound by memory: two splits of 333 x 12288 9.3 us for 41 MB (12.0 with outputs stored one by one).
 template <int EPI>
 __global__ __launch_bounds__(256) void w4_join_kernel(W4Gemm p) {
   constexpr int STEP = epi_is_glu(EPI) ? 2 : 1;
@@ -644,12 +652,20 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Gemm p) {
     for (int s = 0; s < 8; ++s) v += a[s], u += b[s];
   }
   const float f = p.factor[m];
+  const f32x4 n0 = *reinterpret_cast<const f32x4*>(p.col_norm + c);
+  f32x4 n1 = n0;
+  if constexpr (STEP == 2) n1 = *reinterpret_cast<const f32x4*>(p.col_norm + c + 16);
+  float o[4];
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    if (n + e >= p.ncols) break;
-    const float bias = EPI == EPI_RMS && p.bias ? p.bias[n + e] : 0.0f;
-    const float f1 = STEP == 2 ? 1.0f / p.col_norm[c + e + 16] : 0.0f;
-    p.y[m * p.ldy + n + e] = (__bf16)w4_value<EPI>(v[e] / p.col_norm[c + e], u[e] * f1, f, bias);
+    const float bias = EPI == EPI_RMS && p.bias && n + e < p.ncols ? p.bias[n + e] : 0.0f;
+    o[e] = w4_value<EPI>(v[e] * (1.0f / n0[e]), u[e] * (1.0f / n1[e]), f, bias);
+  }
+  __bf16* dst = p.y + m * p.ldy + n;
+  if (n + 4 <= p.ncols) {
+    *reinterpret_cast<u32x2*>(dst) = pack4_bf16(o);
+  } else {
+    for (int e = 0; n + e < p.ncols; ++e) dst[e] = (__bf16)o[e];
   }
 }
 
