@@ -626,7 +626,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
 }
 
 // Joins the splits of K in order and applies the epilogue: one thread per four packed columns of a row (GLU:
-// four gate columns and their up columns).  Bound by memory: two splits of 333 x 12288 9.3 us for 41 MB (12.0 with outputs stored one by one).
+// four gate columns and their up columns).  Bound by memory: two splits of 333 x 12288 9.3 us for 41 MB (12.0 with
+// the outputs stored one by one).
 template <int EPI>
 __global__ __launch_bounds__(256) void w4_join_kernel(W4Gemm p) {
   constexpr int STEP = epi_is_glu(EPI) ? 2 : 1;
