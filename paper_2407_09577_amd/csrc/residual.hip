@@ -201,8 +201,8 @@ Units units_of(int64_t M, int64_t gate_rows, bool gate, int tpr) {
 // Rows of more than a vector a thread (more than 8192 bf16 or 4096 fp32 columns) are read three times: 3.1 TB/s of
 // their bytes in bf16, 5.1 (4096 columns), 4.0 (8192) and 2.7 (16384) in fp32.
 template <typename T, int TPR, int V, bool POST, bool PRE>
-__global__ __launch_bounds__(TPR, TPR >= 512 ? 4 : 1) void residual_bwd_kernel(ResidualArgs p, Units un, float* part_post, float* part_pre,
-                                                           float* part_gate) {
+__global__ __launch_bounds__(TPR, TPR >= 512 ? 4 : 1) void residual_bwd_kernel(ResidualArgs p, Units un, float* part_post,
+                                                                               float* part_pre, float* part_gate) {
   constexpr int VN = Vec<T>::N;
   __shared__ float buf1[2][1][TPR / 64];
   __shared__ float buf5[2][5][TPR / 64];

@@ -213,7 +213,8 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t* __restrict_
   scales[grp * NPB * 16 + cb * 16 + (lane & 15)] = word;
 }
 
-// After the scales, in a launch of 1.6 to 4 us.  The power of two that brings a packed column's largest |s| into [2^9, 2^10): sixteen threads per column.
+// The power of two that brings a packed column's largest |s| into [2^9, 2^10): sixteen threads per column, a launch of
+// 1.6 to 4 us behind the one that writes the scales.
 __global__ __launch_bounds__(256) void w4_norms_kernel(const unsigned* __restrict__ scales, int64_t groups, int64_t NP,
                                                        float* __restrict__ norms) {
   __shared__ unsigned red[16][16];
