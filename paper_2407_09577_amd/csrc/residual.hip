@@ -174,10 +174,13 @@ struct Units {
 };
 
 // Enough units to fill the chip (eight waves per SIMD for narrow rows, four for wide), and no more: each
-// leaves a row of fp32 partial sums per parameter.
+// leaves a row of fp32 partial sums per parameter.  A few rows are one unit, whose sums are the whole, so that no
+// second launch adds them up (10 us in all for 2 to 16 rows of up to 4096): a row more takes 1.2 us with 64 threads
+// (512 columns, 6 rows: 8.9 us), 2.1 with 512 (4096 columns, 3 rows: 8.8) and 7.6 with 1024 and two vectors each.
 Units units_of(int64_t M, int64_t gate_rows, bool gate, int tpr) {
   const int64_t most = tpr <= 128 ? 2048 : tpr == 256 ? 1024 : 512;
   if (M == 0) return Units{0, 0, 0};
+  if (M <= (tpr <= 128 ? 6 : tpr <= 512 ? 3 : 1)) return Units{1, (int)M, 0};
   int64_t rows = (M + most - 1) / most;
   if (!gate || gate_rows == 1) return Units{(M + rows - 1) / rows, (int)rows, 0};
   const int64_t segs = (M + gate_rows - 1) / gate_rows, T = gate_rows < M ? gate_rows : M;
@@ -460,8 +463,8 @@ hipError_t launch_bwd_t(const ResidualArgs& p) {
     if (wanted) next += un.count * p.K;
     return q;
   };
-  float* part_post = take(p.dg_post != nullptr);
-  float* part_pre = take(p.dg_pre != nullptr);
+  float* part_post = un.count == 1 ? p.dg_post : take(p.dg_post != nullptr);
+  float* part_pre = un.count == 1 ? p.dg_pre : take(p.dg_pre != nullptr);
   float* part_gate = take(p.dgate && un.pieces);
   if (un.count) {
     const hipError_t e = with_shape<T>(p.K, [&](auto tpr, auto v) {
@@ -475,6 +478,7 @@ hipError_t launch_bwd_t(const ResidualArgs& p) {
     });
     if (e != hipSuccess) return e;
   }
+  if (un.count == 1) return hipSuccess;
   const unsigned sums = (p.dg_post ? 1 : 0) + (p.dg_pre ? 1 : 0) + (part_gate ? (unsigned)(un.count / un.pieces) : 0);
   if (!sums) return hipSuccess;
   hipLaunchKernelGGL(residual_sums_kernel<T>, dim3((p.K + 31) / 32, sums), dim3(256), 0, p.stream, p, un, part_post, part_pre,
