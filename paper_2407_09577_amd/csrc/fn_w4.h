@@ -38,11 +38,23 @@ constexpr unsigned kW4ScaleMask = 0xfffff000u;
 // Bit of code e (0..7) in its word.
 __device__ __forceinline__ constexpr int w4_bit(int e) { return 4 * (e >> 1) + 16 * (e & 1); }
 
-// The eight codes of a word as bf16 128 + q, in k order.
-__device__ __forceinline__ bf16x8 w4_widen(unsigned w) {
+// The and-or's operands in registers, a scalar and a vector one: with literals, which it cannot take, it becomes two
+// instructions, and the widening is what the products' vector units do most (the few-row kernel at 64 x 11008 -> 4096:
+// 18.6 us with literals, 17.7 so).
+struct W4Bits {
+  unsigned low, high, bias;
+  __device__ __forceinline__ explicit W4Bits(unsigned b) : low(0x000f000fu), high(0x00f000f0u), bias(b) {
+    asm("" : "+s"(low));
+    asm("" : "+s"(high));
+    asm("" : "+v"(bias));
+  }
+};
+
+// The eight codes of a word as bf16 128 + q, in k order (the bias: 0x43004300).
+__device__ __forceinline__ bf16x8 w4_widen(unsigned w, const W4Bits& k) {
   u32x4 r;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = ((w >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+  for (int i = 0; i < 4; ++i) r[i] = ((w >> (4 * i)) & k.low) | k.bias;
   return __builtin_bit_cast(bf16x8, r);
 }
 

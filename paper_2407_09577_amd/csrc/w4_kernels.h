@@ -79,6 +79,8 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
   const unsigned one2 = 0x3f803f80u;  // bf16 1, twice
   const bf16x8 ones = __builtin_bit_cast(bf16x8, u32x4{one2, one2, one2, one2});
 
+  const W4Bits bits(0x43004300u);
+
   struct Set {
     u32x4 w[NCB], a[RG][4], g[GS ? 2 : 1];
     unsigned s[NG][NCB];
@@ -173,7 +175,7 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
         for (int q = 0; q < RG; ++q) part[q] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int b = 0; b < GB; ++b) {
-          const bf16x8 wv = w4_widen(t.w[c][j * GB + b]);
+          const bf16x8 wv = w4_widen(t.w[c][j * GB + b], bits);
           if constexpr (GS) part[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(al[b], wv, part[0], 0, 0, 0);
 #pragma unroll
           for (int q = 0; q < RG; ++q) part[q] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(av[q][b], wv, part[q], 0, 0, 0);
@@ -362,13 +364,14 @@ __global__ __launch_bounds__(T) void w4_rows_kernel(const __bf16* __restrict__ a
 
 // The eight weights of a word as fp16 (q - z) r, in k order.  zero holds 1024 + z twice, r and r16 the
 // group's scale and a sixteenth of it: the odd nibbles are taken where they stand, as 16 q.
-__device__ __forceinline__ f16x8 w4_widen_f16(unsigned w, f16x2 zero, f16x2 zero16, f16x2 r, f16x2 r16) {
+__device__ __forceinline__ f16x8 w4_widen_f16(unsigned w, const W4Bits& k, f16x2 zero, f16x2 zero16, f16x2 r,
+                                               f16x2 r16) {
   auto at = [](unsigned v) { return __builtin_bit_cast(f16x2, v); };
   const unsigned h = w >> 8;
-  const f16x2 p0 = (at((w & 0x000f000fu) | 0x64006400u) - zero) * r;
-  const f16x2 p1 = (at((w & 0x00f000f0u) | 0x64006400u) - zero16) * r16;
-  const f16x2 p2 = (at((h & 0x000f000fu) | 0x64006400u) - zero) * r;
-  const f16x2 p3 = (at((h & 0x00f000f0u) | 0x64006400u) - zero16) * r16;
+  const f16x2 p0 = (at((w & k.low) | k.bias) - zero) * r;
+  const f16x2 p1 = (at((w & k.high) | k.bias) - zero16) * r16;
+  const f16x2 p2 = (at((h & k.low) | k.bias) - zero) * r;
+  const f16x2 p3 = (at((h & k.high) | k.bias) - zero16) * r16;
   return f16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
 
@@ -470,6 +473,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
     for (int c = 0; c < NCB; ++c) acc[t][c] = f32x4{0.f, 0.f, 0.f, 0.f};
 
   const int rbase = (kg * ROWS + wm * MB * 16 + lrow) * 256;
+  const W4Bits bits(0x64006400u);
   auto compute = [&](int st, const Weights& t) __attribute__((always_inline)) {
     const char* stage = smem + st * STAGE + rbase;
     auto zero_of = [&](int j, int c) __attribute__((always_inline)) {
@@ -498,7 +502,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
       const f16x2 r1 = NG < 4 ? r[NG < 4 ? u / GB : 0][c] : scale_of(u / GB, c);
       // 1024 + 16 z = 16 (1024 + z) - 15 * 1024, exactly
       const f16x2 z16 = (z1 - f16x2{1024, 1024}) * f16x2{16, 16} + f16x2{1024, 1024};
-      wv[u & 1][c] = w4_widen_f16(t.w[c][u], z1, z16, r1, r1 * f16x2{0.0625, 0.0625});
+      wv[u & 1][c] = w4_widen_f16(t.w[c][u], bits, z1, z16, r1, r1 * f16x2{0.0625, 0.0625});
     };
     auto read = [&](int s) __attribute__((always_inline)) {
       av[s % D] = *reinterpret_cast<const f16x8*>(stage + s % MB * 4096 + (((4 * (s / MB) + lch) ^ lrow) * 16));
