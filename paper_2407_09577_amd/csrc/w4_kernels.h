@@ -44,9 +44,10 @@ __device__ __forceinline__ void split_ag(const bf16x8& a, const f32x4& g0, const
 // along the rows and turned in a slot of LDS of its own.  That halves the requests of a load of sixteen rows
 // (4096 -> 6144 with one column block a wave: 11.9 -> 9.1 us) and only adds a wait to one of a row or two
 // (two blocks: 6.6 -> 7.6).
-// Kernel times: 1 x 4096 -> 6144 6.9 us, 16 x 4096 -> 22016 GLU 14.5 us for 50 MB, beside 3.1 us of a kernel that does
-// nothing: the stream itself runs at 3.5 to 4.4 TB/s.  64 x 11008 -> 4096 (18.6 us a call) is bound by the widening,
-// once for each 16 rows, and its waits; the matrix cores are busy for 11% of it.
+// Kernel times: 1 x 4096 -> 6144 6.8 us, 16 x 4096 -> 22016 GLU 13.8 us for 50 MB, beside 3.1 us of a kernel that does
+// nothing: the stream itself runs at 3.7 to 4.7 TB/s.  64 x 11008 -> 4096 (17.7 us a call) is bound by the widening,
+// once for each 16 rows, and its waits; the matrix cores are busy for an eighth of it.  Loads two blocks ahead gained 5%
+// at K = 11008 and cost as much at 4096.
 template <int NCB, int KS, int RG, int GB, int EPI, bool GS, bool STAGED>
 __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restrict__ a, int M, int K, int lda,
                                                          const void* __restrict__ codes,
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
 // past K, and the factor that the outputs take: (1 / RMSe, or the given row scale) / the power of two.
 // With g the values are a g, rounded to fp16.  A row that holds a NaN or an infinity gets a NaN factor.
 // T threads hold up to H pieces of 16 bytes each; H = 0: the row is read twice.  Bound by its launch and one trip to
-// memory: 333 x 4096 5.2 us.
+// memory: 333 x 4096 5.2 us, 2048 x 4096 10.5 us.
 template <bool NORM, int T, int H>
 __global__ __launch_bounds__(T) void w4_rows_kernel(const __bf16* __restrict__ a, int K, int lda,
                                                     const float* __restrict__ g, const float* __restrict__ row_scale,
@@ -382,7 +383,7 @@ __device__ __forceinline__ f16x8 w4_widen_f16(unsigned w, const W4Bits& k, f16x2
 // position j ^ (r % 16), so that the sixteen rows of an operand read lie in different banks.
 // With several `splits` of K each workgroup writes its fp32 sums and w4_join_kernel finishes them.
 // Bound by the matrix cores where there are enough workgroups, else by the waits in one set: 2048 x 4096 -> 22016 GLU
-// 321 us, 1.15 PFLOP/s with the matrix cores busy for half of the time; a set of 128 k takes a workgroup that is alone
+// 321 us (337 on another box), 1.10 to 1.15 PFLOP/s with the matrix cores busy for half of the time; a set of 128 k takes a workgroup that is alone
 // on its compute unit 2600 cycles, 1024 of them matrix-core operations.  Weights through LDS as well, a third stage,
 // operands read six or eight steps ahead and widening spread over the steps, into the next set's first, did not help.
 struct W4Gemm {
