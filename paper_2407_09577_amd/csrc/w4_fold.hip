@@ -17,8 +17,8 @@ __device__ __forceinline__ double twelve_bits(double s) {
 __device__ __forceinline__ double w4_span(double lo, double hi, bool zero_points) {
   return zero_points ? (hi - lo) / 15.0 : fmax(-lo, hi) / 7.0;
 }
-__device__ __forceinline__ void w4_scale_of(double lo, double hi, bool bad, bool zero_points, float& s, float& z) {
-  const double d = twelve_bits(w4_span(lo, hi, zero_points));
+__device__ __forceinline__ void w4_scale_of(double span, double lo, bool bad, bool zero_points, float& s, float& z) {
+  const double d = twelve_bits(span);
   s = bad || !(d <= 0x1.fffffep127) ? __builtin_nanf("") : d < 0x1p-126 ? 0.0f : (float)d;
   z = zero_points && s > 0.0f ? (float)fmin(fmax(rint(-lo / d), 0.0), 15.0) : 8.0f;
 }
@@ -52,6 +52,12 @@ __device__ __forceinline__ void w4_put(u32x4& out, int u, int e, unsigned q) {
   for (int i = 0; i < 4; ++i) out[i] = i == u ? (out[i] & ~(15u << shift)) | q << shift : out[i];
 }
 
+// The power of two that brings a largest |s| with these bits into [2^9, 2^10).
+__device__ __forceinline__ float w4_norm_of(unsigned top) {
+  const unsigned ex = top >> 23;  // 255: a column that holds no finite scale stays as it is
+  return ex == 255u || top == 0u ? 1.0f : __uint_as_float(min(263u - ex, 254u) << 23);
+}
+
 // One wave quantises a code fragment: lane 16 c + p holds 32 k of column p, so a group's smallest and largest
 // product meet across the four lanes of a column.  By definition g w is exact, the scale is rounded once from
 // the extremes and the code is the nearest one to the fp64 quotient, so the result does not depend on the order
@@ -63,23 +69,28 @@ __device__ __forceinline__ void w4_put(u32x4& out, int u, int e, unsigned q) {
 //   right one unless it is that near to a half (one weight in 130000: decided again in fp64).
 // Groups whose largest product is not between 2^-100 and 2^100 are taken in fp64 throughout, but for zeros.
 // Bound by memory and, nearly as much, by the arithmetic: about ten operations a weight.  4096 x 22016 bf16 from
-// [N, K]: 114 us with fp64 quotients throughout, 78 to 89 us so, for 228 MB.
-template <typename T, int GB>
-__global__ __launch_bounds__(256) void w4_fold_kernel(const T* __restrict__ W, int64_t sk, int64_t sn, int64_t K,
-                                                      int64_t N, const float* __restrict__ g, int glu, bool vec,
-                                                      bool gvec, bool zero_points, int NPB, int KB, int kgroups,
-                                                      u32x4* __restrict__ codes, unsigned* __restrict__ scales) {
+// [N, K]: 114 us with fp64 quotients throughout, 65 to 90 us so (on different boxes), for 228 MB.
+// A workgroup takes cw column and kw k blocks.  Of the four lanes of a column each makes the scale of one group, if
+// there are as many: made by each lane in turn, four groups' fp64 took 3 us of a small fold and a fifth of a large
+// one (4096 x 22016, groups of 32: 91 us a call, 73 so).  WHOLE: kw is all of K, so the workgroup sees whole columns
+// and writes their norms too, and no second launch reads the scales (576 x 1536: 12.2 us a call in all, 9.0 so).
+template <typename T, int GB, bool WHOLE>
+__global__ __launch_bounds__(WHOLE ? 1024 : 256) void w4_fold_kernel(
+    const T* __restrict__ W, int64_t sk, int64_t sn, int64_t K, int64_t N, const float* __restrict__ g, int glu, bool vec,
+    bool gvec, bool zero_points, int NPB, int KB, int cw, int kw, int kgroups, u32x4* __restrict__ codes,
+    unsigned* __restrict__ scales, float* __restrict__ norms) {
   constexpr int NG = 4 / GB;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane >> 4;
-  const int cq = blockIdx.x / kgroups, kq = blockIdx.x % kgroups;
-  const int cb = sk == 1 ? cq : 4 * cq + wave, kb = sk == 1 ? 4 * kq + wave : kq;
-  if (cb >= NPB || kb >= KB) return;
-  const W4Source<T> src{W, sk, sn, K, logical_col((int64_t)cb * 16 + (lane & 15), N, glu), (int64_t)kb * kW4KB + 8 * c, g,
-                        vec, gvec};
-  float p[4][8], s[NG], z[NG], low[NG], high[NG];
+  __shared__ unsigned tops[WHOLE ? 16 : 1][16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane >> 4, p16 = lane & 15;
+  const int cb = (int)(blockIdx.x / kgroups) * cw + wave % cw, kb = (int)(blockIdx.x % kgroups) * kw + wave / cw;
+  const bool live = cb < NPB && kb < KB;  // else zeros, which only the barrier needs
+  if (!WHOLE && !live) return;
+  const W4Source<T> src{W, sk, sn, K, logical_col((int64_t)cb * 16 + p16, N, glu), (int64_t)kb * kW4KB + 8 * c, g, vec,
+                        gvec};
+  const int mine = c & (NG - 1);
+  float p[4][8], low[NG], high[NG], lo_m = 0.0f, hi_m = 0.0f, any_m = 0.0f;
 #pragma unroll
   for (int u = 0; u < 4; ++u) src.products(u, p[u]);
-  bool near = false, far = false;
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
     float lo = 0.0f, hi = 0.0f, any = 0.0f;
@@ -98,18 +109,22 @@ __global__ __launch_bounds__(256) void w4_fold_kernel(const T* __restrict__ W, i
       any += __shfl_xor(any, o);
     }
     low[j] = lo, high[j] = hi;
-    const double span = w4_span(lo, hi, zero_points);
-    const float top = fmaxf(-lo, hi), q = zero_points ? lo / (float)span : 0.0f;
-    w4_scale_of(lo, hi, false, zero_points, s[j], z[j]);
-    far |= any != any || !(top == 0.0f || (top >= 0x1p-100f && top <= 0x1p100f));
-    near |= top > 0.0f && (twelve_bits(span * (1.0 - 0x1p-23)) != twelve_bits(span * (1.0 + 0x1p-23)) ||
-                           fabsf(q - rintf(q)) > 0.5f - 0x1p-12f);  // q from the unrounded span: 2^-12 off
+    if (j == mine) lo_m = lo, hi_m = hi, any_m = any;
   }
-  if (__any(near | far)) {
+  const double span = w4_span(lo_m, hi_m, zero_points);
+  const float top = fmaxf(-lo_m, hi_m), q0 = zero_points ? lo_m / (float)span : 0.0f;
+  float s_m, z_m;
+  w4_scale_of(span, lo_m, false, zero_points, s_m, z_m);
+  const bool far_m = any_m != any_m || !(top == 0.0f || (top >= 0x1p-100f && top <= 0x1p100f));
+  const bool near_m =
+      top > 0.0f && (twelve_bits(span * (1.0 - 0x1p-23)) != twelve_bits(span * (1.0 + 0x1p-23)) ||
+                     fabsf(q0 - rintf(q0)) > 0.5f - 0x1p-12f);  // q0 from the unrounded span: 2^-12 off
+  if (__any(near_m | far_m)) {
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
+      if (!__any(mine == j && (near_m | far_m))) continue;
       // Rounding keeps the order: the exact extremes are among the products that round to the extremes.
-      unsigned at = far ? 0xffffffffu : 0;
+      unsigned at = (NG == 1 ? (int)far_m : __shfl((int)far_m, p16 + 16 * j)) ? 0xffffffffu : 0;
 #pragma unroll
       for (int u = j * GB; u < (j + 1) * GB; ++u)
 #pragma unroll
@@ -132,9 +147,20 @@ __global__ __launch_bounds__(256) void w4_fold_kernel(const T* __restrict__ W, i
         hi = fmax(hi, __shfl_xor(hi, o));
         bad |= __shfl_xor((int)bad, o) != 0;
       }
-      w4_scale_of(lo, hi, bad, zero_points, s[j], z[j]);
+      float sj, zj;
+      w4_scale_of(w4_span(lo, hi, zero_points), lo, bad, zero_points, sj, zj);
+      if (j == mine) s_m = sj, z_m = zj;
     }
   }
+  float s[NG], z[NG];
+#pragma unroll
+  for (int j = 0; j < NG; ++j) {
+    s[j] = NG == 1 ? s_m : __shfl(s_m, p16 + 16 * j);
+    z[j] = NG == 1 ? z_m : __shfl(z_m, p16 + 16 * j);
+  }
+  int far = far_m;
+  if constexpr (NG > 1) far |= __shfl_xor(far, 16);
+  if constexpr (NG > 2) far |= __shfl_xor(far, 32);
   u32x4 out;
   unsigned again = 0;  // bit 8 u + e: the code is to be decided in fp64
 #pragma unroll
@@ -169,12 +195,21 @@ __global__ __launch_bounds__(256) void w4_fold_kernel(const T* __restrict__ W, i
     const double q = sj > 0.0f ? fmin(fmax(rint(src.exact(u, e) / (double)sj) + (double)zj, 0.0), 15.0) : (double)zj;
     w4_put(out, u, e, (unsigned)(int)q);
   }
-  if (lane < 16) {
-#pragma unroll
-    for (int j = 0; j < NG; ++j)
-      scales[((int64_t)kb * NG + j) * NPB * 16 + cb * 16 + lane] = (__float_as_uint(s[j]) & kW4ScaleMask) | (unsigned)z[j];
+  const unsigned word = (__float_as_uint(s_m) & kW4ScaleMask) | (unsigned)z_m;
+  if (live) {
+    if (c < NG) scales[((int64_t)kb * NG + c) * NPB * 16 + cb * 16 + p16] = word;
+    codes[((int64_t)kb * NPB + cb) * 64 + lane] = out;
   }
-  codes[((int64_t)kb * NPB + cb) * 64 + lane] = out;
+  if constexpr (WHOLE) {
+    unsigned most = word & 0x7ffff000u;
+    most = max(most, (unsigned)__shfl_xor((int)most, 16));
+    most = max(most, (unsigned)__shfl_xor((int)most, 32));
+    if (lane < 16) tops[wave][lane] = most;
+    __syncthreads();
+    if (wave >= cw || lane >= 16 || cb >= NPB) return;
+    for (int k = 1; k < kw; ++k) most = max(most, tops[k * cw + wave][lane]);
+    norms[cb * 16 + lane] = w4_norm_of(most);
+  }
 }
 
 // One wave packs a code fragment, a byte at a time (16 columns of a row lie together): 4096 x 22016 68 us for 140 MB.
@@ -213,8 +248,7 @@ __global__ __launch_bounds__(256) void w4_pack_kernel(const uint8_t* __restrict_
   scales[grp * NPB * 16 + cb * 16 + (lane & 15)] = word;
 }
 
-// The power of two that brings a packed column's largest |s| into [2^9, 2^10): sixteen threads per column, a launch of
-// 1.6 to 4 us behind the one that writes the scales.
+// The norms of columns whose scales other launches or workgroups wrote: sixteen threads per column, 1.6 to 4 us.
 __global__ __launch_bounds__(256) void w4_norms_kernel(const unsigned* __restrict__ scales, int64_t groups, int64_t NP,
                                                        float* __restrict__ norms) {
   __shared__ unsigned red[16][16];
@@ -228,8 +262,7 @@ __global__ __launch_bounds__(256) void w4_norms_kernel(const unsigned* __restric
   if (w) return;
 #pragma unroll
   for (int i = 1; i < 16; ++i) top = max(top, red[i][c]);
-  const unsigned ex = top >> 23;  // 255: a column that holds no finite scale stays as it is
-  norms[col] = ex == 255u || top == 0u ? 1.0f : __uint_as_float(min(263u - ex, 254u) << 23);
+  norms[col] = w4_norm_of(top);
 }
 
 static hipError_t launch_w4_norms(void* w4, int64_t K, int64_t N, int glu, int group, hipStream_t stream) {
@@ -269,15 +302,26 @@ static hipError_t launch_w4_fold_t(const W4FoldArgs& p) {
   auto aligned = [](const void* q) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0; };
   const bool vec = p.sk == 1 && p.K % 8 == 0 && aligned(W) && p.sn * (int64_t)sizeof(T) % 16 == 0;
   const int NPB = (int)(packed_cols(p.N, p.glu) / 16), KB = (int)w4_blocks(p.K);
-  const int kstep = p.sk == 1 ? 4 : 1, cstep = p.sk == 1 ? 1 : 4, kgroups = (KB + kstep - 1) / kstep;
+  // A workgroup takes all blocks of k where sixteen waves have room for them (beside two column blocks where the columns
+  // lie together: with one, 2048 x 8192 in rows took 30.9 us, 18.9 in two launches).  Else four blocks along the
+  // contiguous axis.
+  const bool whole = KB <= (p.sk == 1 ? 16 : 8);
+  const int cw = p.sk == 1 ? 1 : !whole || KB <= 4 ? 4 : 2, kw = whole ? KB : p.sk == 1 ? 4 : 1;
+  const int kgroups = (KB + kw - 1) / kw;
   auto go = [&](auto kernel) {
-    hipLaunchKernelGGL(kernel, dim3((unsigned)kgroups * ((NPB + cstep - 1) / cstep)), dim3(256), 0, p.stream, W, p.sk,
-                       p.sn, p.K, p.N, p.g, p.glu, vec, aligned(p.g), p.zero_points, NPB, KB, kgroups,
-                       reinterpret_cast<u32x4*>(p.w4), w4_scales(p.w4, p.K, p.N, p.glu));
+    hipLaunchKernelGGL(kernel, dim3((unsigned)kgroups * ((NPB + cw - 1) / cw)), dim3(64 * cw * kw), 0, p.stream, W, p.sk,
+                       p.sn, p.K, p.N, p.g, p.glu, vec, aligned(p.g), p.zero_points, NPB, KB, cw, kw, kgroups,
+                       reinterpret_cast<u32x4*>(p.w4), w4_scales(p.w4, p.K, p.N, p.glu),
+                       w4_norms(p.w4, p.K, p.N, p.glu, p.group));
     const hipError_t e = hipGetLastError();
-    return e == hipSuccess ? launch_w4_norms(p.w4, p.K, p.N, p.glu, p.group, p.stream) : e;
+    return e != hipSuccess || whole ? e : launch_w4_norms(p.w4, p.K, p.N, p.glu, p.group, p.stream);
   };
-  return p.group == 32 ? go(w4_fold_kernel<T, 1>) : p.group == 64 ? go(w4_fold_kernel<T, 2>) : go(w4_fold_kernel<T, 4>);
+  if (whole) {
+    if (p.group == 32) return go(w4_fold_kernel<T, 1, true>);
+    return p.group == 64 ? go(w4_fold_kernel<T, 2, true>) : go(w4_fold_kernel<T, 4, true>);
+  }
+  if (p.group == 32) return go(w4_fold_kernel<T, 1, false>);
+  return p.group == 64 ? go(w4_fold_kernel<T, 2, false>) : go(w4_fold_kernel<T, 4, false>);
 }
 
 hipError_t launch_w4_fold(const W4FoldArgs& p) {

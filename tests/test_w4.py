@@ -463,3 +463,28 @@ def test_fold_on_another_stream(fn):
     got = fn.unpack_weights_w4(w4, stream=side.cuda_stream)
     side.synchronize()
     assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("K,N,rows,glu", [(8, 1, True, False), (300, 75, True, False), (512, 190, False, True), (600, 74, True, True),
+                                          (1024, 66, True, False), (1032, 40, True, False), (2048, 33, False, False),
+                                          (2049, 34, False, True), (4100, 70, True, True)])
+def test_columns_norms(fn, K, N, rows, glu, group):
+    """The power of two behind each packed column of a fold: its largest scale lies in [2^9, 2^10) times it, one for
+    columns without a finite scale (padding, zeros, NaN)."""
+    gen = torch.Generator().manual_seed(K + N)
+    W = torch.randn(K, N, generator=gen) * torch.exp2(torch.randint(-40, 40, (1, N), generator=gen).float())
+    if N > 3:
+        W[:, 1] = 0.0
+        W[K // 2, 2] = float("nan")
+    W = W if rows else W.t().contiguous().t()
+    w4 = fn.fold_weights_w4(W.to(DEV), layout=fn.FN_LAYOUT_GLU if glu else fn.FN_LAYOUT_LINEAR, group=group)
+    NP = 2 * (-(-(N // 2) // 16) * 16) if glu else -(-N // 16) * 16
+    groups = -(-K // 128) * (128 // group)
+    tail = w4.data.cpu()[-4 * NP * (groups + 1):]
+    words, norms = tail[:4 * NP * groups].view(torch.int32).view(groups, NP), tail[4 * NP * groups:].view(torch.float32).numpy()
+    top = (words & 0x7ffff000).view(torch.float32).abs().numpy()
+    bad = ~np.isfinite(top).all(0) | (top.max(0) == 0)
+    assert (norms[bad] == 1.0).all() and bad.sum() >= (2 if N > 3 else 0)
+    e = np.frexp(top.max(0)[~bad])[1]
+    assert np.array_equal(norms[~bad], np.ldexp(1.0, 10 - e).astype(np.float32))
