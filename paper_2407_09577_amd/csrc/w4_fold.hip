@@ -72,8 +72,8 @@ __device__ __forceinline__ float w4_norm_of(unsigned top) {
 // [N, K]: 114 us with fp64 quotients throughout, 65 to 90 us so (on different boxes), for 228 MB.
 // A workgroup takes cw column and kw k blocks.  Of the four lanes of a column each makes the scale of one group, if
 // there are as many: made by each lane in turn, four groups' fp64 took 3 us of a small fold and a fifth of a large
-// one (4096 x 22016, groups of 32: 91 us a call, 73 so).  WHOLE: kw is all of K, so the workgroup sees whole columns
-// and writes their norms too, and no second launch reads the scales (576 x 1536: 12.2 us a call in all, 9.0 so).
+// one (4096 x 22016, groups of 32: 91 us a call, 71 so).  WHOLE: kw is all of K, so the workgroup sees whole columns
+// and writes their norms too, and no second launch reads the scales (576 x 1536: 12.2 us a call in all, 8.1 so).
 template <typename T, int GB, bool WHOLE>
 __global__ __launch_bounds__(WHOLE ? 1024 : 256) void w4_fold_kernel(
     const T* __restrict__ W, int64_t sk, int64_t sn, int64_t K, int64_t N, const float* __restrict__ g, int glu, bool vec,
@@ -81,8 +81,11 @@ __global__ __launch_bounds__(WHOLE ? 1024 : 256) void w4_fold_kernel(
     unsigned* __restrict__ scales, float* __restrict__ norms) {
   constexpr int NG = 4 / GB;
   __shared__ unsigned tops[WHOLE ? 16 : 1][16];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane >> 4, p16 = lane & 15;
-  const int cb = (int)(blockIdx.x / kgroups) * cw + wave % cw, kb = (int)(blockIdx.x % kgroups) * kw + wave / cw;
+  const int lane = threadIdx.x & 63, c = lane >> 4, p16 = lane & 15;
+  const int wave = WHOLE ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : threadIdx.x >> 6;
+  const int cq = blockIdx.x / kgroups, kq = blockIdx.x % kgroups;
+  const int cb = WHOLE ? cq * cw + wave % cw : cw == 1 ? cq : 4 * cq + wave;
+  const int kb = WHOLE ? wave / cw : cw == 1 ? 4 * kq + wave : kq;
   const bool live = cb < NPB && kb < KB;  // else zeros, which only the barrier needs
   if (!WHOLE && !live) return;
   const W4Source<T> src{W, sk, sn, K, logical_col((int64_t)cb * 16 + p16, N, glu), (int64_t)kb * kW4KB + 8 * c, g, vec,

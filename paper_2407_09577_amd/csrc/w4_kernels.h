@@ -708,7 +708,8 @@ static hipError_t launch_w4_few_g(const W4Args& p, int shape) {
   }
   if constexpr (!epi_is_glu(EPI)) {
     if (shape == 7) return launch_w4_few_cfg<1, 8, 1, GB, EPI, GS>(p);
-    if (shape == 8) return launch_w4_few_cfg<1, 16, 1, GB, EPI, GS>(p);
+    if constexpr (!GS)
+      if (shape == 8) return launch_w4_few_cfg<1, 16, 1, GB, EPI, GS>(p);
     if (shape == 9) return launch_w4_few_cfg<3, 8, 1, GB, EPI, GS>(p);
   }
   return hipErrorInvalidValue;

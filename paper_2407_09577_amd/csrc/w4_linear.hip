@@ -24,6 +24,9 @@ extern template hipError_t launch_w4_many<EPI_ROWSCALE>(const W4Gemm&, int, int,
 // widening: where a call has no more than a workgroup for each, two or eight k groups do (695 x 3928 x 3520:
 // 42.4 us with 96 x 128 tiles, 35.2 with two k groups on each).  Two blocks of rows on a few-row workgroup widen the
 // codes once for both, where the width alone fills the chip (32 x 4096 -> 22016 GLU: 21.5 us with one, 18.6 with two).
+// The few-row kernel is not for few rows alone: narrow products of many rows take it too, which spares them the pass over
+// the rows and the join (500 x 1024 -> 1024 9.3 -> 5.9 us, 432 x 5720 -> 284 16.5 -> 10.5, 1269 x 2328 -> 384
+// 14.0 -> 9.6).
 struct W4Shape {
   int rows, cols, ks, per_cu;
   float start, full, one, each;
@@ -44,8 +47,6 @@ static constexpr W4Shape kW4Many[] = {
 constexpr int kW4FewLinearOnly = 7;  // from here on: an odd number of column blocks holds no gate/up pairs
 constexpr float kW4FewUs = 4.15f, kW4FewPerMK = 0.915f;
 constexpr float kW4ManyUs = 7.14f, kW4ManyPerMK = 0.859f, kW4JoinUs = 3.04f, kW4JoinPerMB = 0.255f;
-// The few-row kernel reads its rows once per column tile and is not looked at beyond this many.
-constexpr int kW4FewMaxM = 256;
 
 // A non-negative x rounded up (ceilf would be a call).
 static float up(float x) {
@@ -67,15 +68,17 @@ struct W4Best {
 };
 
 // Smaller groups and a run-time g cost the few-row kernel most: a scale, a sum and four multiply-adds per group and
-// column, and two matrix-core operations for one.  Measured at 16..128 rows as factors of the shapes' times.
+// column, and two matrix-core operations for one.  Measured at 150..1269 rows as factors of the shapes' times (1.35 to 1.6
+// for groups of 32, 1.15 to 1.25 for 64; with g 1.4 to 1.9).
 static W4Best few_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs) {
   W4Best best{{false, 0, 1, KB}, 1e30f};
-  if (M > kW4FewMaxM) return best;
-  const float x = (group == 32 ? 1.55f : group == 64 ? 1.2f : 1.0f) * (gs ? 1.9f : 1.0f);
+  const float x = (group == 32 ? 1.45f : group == 64 ? 1.18f : 1.0f) * (gs ? 1.6f : 1.0f);
   for (int i = 0; i < (glu ? kW4FewLinearOnly : (int)(sizeof(kW4Few) / sizeof(W4Shape))); ++i) {
     const W4Shape& s = kW4Few[i];
-    // Beside two blocks of rows there are no registers for a g's halves, nor for six columns' scales of small groups.
-    if (s.rows == 32 && (M <= 16 || gs || (s.cols == 96 && group < 128))) continue;
+    // Beside two blocks of rows, and in sixteen waves, there are no registers for a g's halves; nor, beside the former,
+    // for six columns' scales of small groups.
+    if (gs && (s.rows == 32 || s.ks == 16)) continue;
+    if (s.rows == 32 && (M <= 16 || (s.cols == 96 && group < 128))) continue;
     const int64_t wgs = (int64_t)((M + s.rows - 1) / s.rows) * ((NP + s.cols - 1) / s.cols);
     const float us = kW4FewUs + kW4FewPerMK * ((float)M * (float)K * 1e-6f) + x * shape_us(s, wgs, (KB + s.ks - 1) / s.ks);
     if (us < best.us) best = W4Best{{false, i, 1, KB}, us};

@@ -348,7 +348,7 @@ def test_a_feed_forward_block(fn):
 
 def test_workspace(fn):
     """A caller's workspace, one for several calls; what lies behind it stays as it was."""
-    K, N = 512, 320
+    K, N = 512, 4000
     codes, scales, z = weights(K, N, 64, True, 11)
     w4 = fn.pack_weights_w4(codes.to(DEV), scales.to(DEV), z.to(DEV), group=64)
     need = {M: fn.lib().flashnorm_w4_workspace_size(M, K, N, 0, 64) for M in (1, 16, 300, 2000)}

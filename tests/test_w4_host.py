@@ -61,12 +61,13 @@ def test_products_refuse(lib):
     assert _lin(lib, lda=1 << 22) == -9
     big = dict(M=1 << 30, K=8, lda=8, N=1 << 20, ldy=1 << 20, y=1 << 60)
     assert _lin(lib, ws=1 << 61, wb=1 << 59, **big) == -9   # more workgroups than a launch takes
-    assert _lin(lib, M=1000) == -1                          # a workspace is needed
-    need = lib.flashnorm_w4_workspace_size(1000, 64, 32, 0, 32)
-    assert need > 1000 * 64 * 2
-    assert _lin(lib, M=1000, ws=B, wb=need - 1) == -9
-    assert _lin(lib, M=1000, ws=B + 8, wb=need) == -4
-    assert _lin(lib, M=1000, ws=Y, wb=need) == -8 and _lin(lib, M=1000, ws=A, wb=need) == -8
+    wide = dict(M=1000, K=1024, lda=1024, N=8192, ldy=8192)   # such calls need a workspace
+    assert _lin(lib, **wide) == -1
+    need = lib.flashnorm_w4_workspace_size(1000, 1024, 8192, 0, 32)
+    assert need > 1000 * 1024 * 2
+    assert _lin(lib, ws=B, wb=need - 1, **wide) == -9
+    assert _lin(lib, ws=B + 8, wb=need, **wide) == -4
+    assert _lin(lib, ws=Y, wb=need, **wide) == -8 and _lin(lib, ws=A, wb=need, **wide) == -8
     f = lib.flashnorm_w4_workspace_size
     assert f(16, 4096, 4096, 0, 128) == 0 and f(0, 64, 32, 0, 32) == 0 and f(-1, 64, 32, 0, 32) == 0
     assert f(1000, 64, 31, 1, 32) == 0 and f(1000, 64, 32, 0, 16) == 0
