@@ -439,13 +439,13 @@ int unpack_weights_w4(const void* W4, int64_t K, int64_t N, int layout, int grou
                       int64_t ldo, void* stream);
 
 /* Bytes of workspace that a product of M rows with such a weight needs, with a run-time g or
- * without (0 for few rows, up to FN_W4_FEW_M always, and for invalid arguments).  Host only. */
+ * without (0 where none is needed, up to FN_W4_FEW_M rows always, and for invalid arguments).  Host only. */
 #define FN_W4_FEW_M 16
 size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout, int group);
 
 /* flashnorm_linear, flashnorm_glu and rowscale_linear with a 4-bit weight.  Sums are fp32.  Few
- * rows multiply the codes unrounded and scale a group's sum; many rows multiply a weight that is
- * rounded to 11 bits (at most 2^-11 of it, with its scale's rounding).  Which way a call goes
+ * rows, and narrow products of more, multiply the codes unrounded and scale a group's sum; wide
+ * products of many rows multiply a weight that is rounded to 11 bits (at most 2^-11 of it, with its scale's rounding).  Which way a call goes
  * depends on M, K, N, the layout, the group and the presence of g alone.
  *   a       [M, K] bf16 (fp32: FN_ERR_UNSUPPORTED), any M, K a multiple of 8.
  *   g       optional [K] fp32 norm weight applied at run time, for a weight into which none
