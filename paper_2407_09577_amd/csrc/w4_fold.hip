@@ -1,5 +1,7 @@
 // 4-bit weights: quantising a weight with g folded in, packing codes that a checkpoint brings, and
 // reading the weight back.  Off the hot path, once per weight.
+#include <type_traits>
+
 #include "fn_fold.h"
 #include "fn_launch.h"
 #include "fn_w4.h"
@@ -38,6 +40,13 @@ struct W4Source {
 #pragma unroll
     for (int e = 0; e < 8; ++e) p[e] *= gv[e];
   }
+  // The same from a fragment that lies in LDS, [128][16].
+  __device__ __forceinline__ void products(const T* own, int u, float (&p)[8]) const {
+    float gv[8];
+    load_v8(g, k0 + 32 * u, K, gvec, 1.0f, gv);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) p[e] = widen(own[(32 * u + e) * 16]) * gv[e];
+  }
   // One product, exactly.
   __device__ __forceinline__ double exact(int u, int e) const {
     const int64_t k = k0 + 32 * u + e;
@@ -74,7 +83,7 @@ __device__ __forceinline__ float w4_norm_of(unsigned top) {
 // there are as many: made by each lane in turn, four groups' fp64 took 3 us of a small fold and a fifth of a large
 // one (4096 x 22016, groups of 32: 91 us a call, 71 so).  WHOLE: kw is all of K, so the workgroup sees whole columns
 // and writes their norms too, and no second launch reads the scales (576 x 1536: 12.2 us a call in all, 8.1 so).
-template <typename T, int GB, bool WHOLE>
+template <typename T, int GB, bool WHOLE, bool ROWS>
 __global__ __launch_bounds__(WHOLE ? 1024 : 256) void w4_fold_kernel(
     const T* __restrict__ W, int64_t sk, int64_t sn, int64_t K, int64_t N, const float* __restrict__ g, int glu, bool vec,
     bool gvec, bool zero_points, int NPB, int KB, int cw, int kw, int kgroups, u32x4* __restrict__ codes,
@@ -90,10 +99,42 @@ __global__ __launch_bounds__(WHOLE ? 1024 : 256) void w4_fold_kernel(
   if (!WHOLE && !live) return;
   const W4Source<T> src{W, sk, sn, K, logical_col((int64_t)cb * 16 + p16, N, glu), (int64_t)kb * kW4KB + 8 * c, g, vec,
                         gvec};
+  // ROWS, bf16 with unit column stride: runs of 16 bytes of a row through LDS, each wave its own fragment (zeros past K
+  // and the columns).  4096 x 11008 in rows 40.7 us with a load for each value, 34.3 so; in fp32, where such loads
+  // bring twice the bytes, the two are within 5% of each other either way.
+  constexpr int EL = 16 / sizeof(T), RUNS = 16 / EL;
+  __shared__ __align__(16) T stage[ROWS ? (WHOLE ? 16 : 4) : 1][ROWS ? kW4KB * 16 : 1];
+  if constexpr (ROWS) {
+    const int64_t n = logical_col((int64_t)cb * 16, N, glu);
+    const int64_t left = n < 0 ? 0 : (glu && n < N / 2 ? N / 2 : N) - n;
+    const int run = lane % RUNS;
+    u32x4 v[2 * RUNS];
+#pragma unroll
+    for (int i = 0; i < 2 * RUNS; ++i) {
+      const int row = i * (64 / RUNS) + lane / RUNS;
+      const int64_t k = (int64_t)kb * kW4KB + row;
+      const T* from = W + k * sk + n + run * EL;
+      v[i] = u32x4{0, 0, 0, 0};
+      if (k < K && left >= (run + 1) * EL) {
+        __builtin_memcpy(&v[i], from, 16);
+      } else if (k < K) {
+        T t[EL];
+#pragma unroll
+        for (int e = 0; e < EL; ++e) t[e] = run * EL + e < left ? from[e] : T(0);
+        __builtin_memcpy(&v[i], t, 16);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2 * RUNS; ++i)
+      *reinterpret_cast<u32x4*>(&stage[wave][(i * (64 / RUNS) + lane / RUNS) * 16 + run * EL]) = v[i];
+  }
   const int mine = c & (NG - 1);
   float p[4][8], low[NG], high[NG], lo_m = 0.0f, hi_m = 0.0f, any_m = 0.0f;
 #pragma unroll
-  for (int u = 0; u < 4; ++u) src.products(u, p[u]);
+  for (int u = 0; u < 4; ++u) {
+    if constexpr (ROWS) src.products(stage[wave] + 8 * c * 16 + p16, u, p[u]);
+    else src.products(u, p[u]);
+  }
 #pragma unroll
   for (int j = 0; j < NG; ++j) {
     float lo = 0.0f, hi = 0.0f, any = 0.0f;
@@ -338,12 +379,15 @@ static hipError_t launch_w4_fold_t(const W4FoldArgs& p) {
     const hipError_t e = hipGetLastError();
     return e != hipSuccess || whole ? e : launch_w4_norms(p.w4, p.K, p.N, p.glu, p.group, p.stream);
   };
-  if (whole) {
-    if (p.group == 32) return go(w4_fold_kernel<T, 1, true>);
-    return p.group == 64 ? go(w4_fold_kernel<T, 2, true>) : go(w4_fold_kernel<T, 4, true>);
-  }
-  if (p.group == 32) return go(w4_fold_kernel<T, 1, false>);
-  return p.group == 64 ? go(w4_fold_kernel<T, 2, false>) : go(w4_fold_kernel<T, 4, false>);
+  auto pick = [&](auto gb) {
+    constexpr int GB = decltype(gb)::value;
+    if constexpr (sizeof(T) == 2)
+      if (p.sk != 1 && p.sn == 1)
+        return whole ? go(w4_fold_kernel<T, GB, true, true>) : go(w4_fold_kernel<T, GB, false, true>);
+    return whole ? go(w4_fold_kernel<T, GB, true, false>) : go(w4_fold_kernel<T, GB, false, false>);
+  };
+  if (p.group == 32) return pick(std::integral_constant<int, 1>{});
+  return p.group == 64 ? pick(std::integral_constant<int, 2>{}) : pick(std::integral_constant<int, 4>{});
 }
 
 hipError_t launch_w4_fold(const W4FoldArgs& p) {

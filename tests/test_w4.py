@@ -488,3 +488,19 @@ def test_columns_norms(fn, K, N, rows, glu, group):
     assert (norms[bad] == 1.0).all() and bad.sum() >= (2 if N > 3 else 0)
     e = np.frexp(top.max(0)[~bad])[1]
     assert np.array_equal(norms[~bad], np.ldexp(1.0, 10 - e).astype(np.float32))
+
+
+@pytest.mark.parametrize("group", [32, 128])
+@pytest.mark.parametrize("K,N,lead,glu", [(8, 1, 3, False), (130, 17, 1, False), (1024, 46, 0, True), (1025, 46, 5, True),
+                                          (1400, 130, 0, False), (300, 64, 7, False)])
+def test_fold_of_rows_at_any_offset(fn, K, N, lead, glu, group):
+    """bf16 weights in rows (unit column stride) that start at any element, amid NaN that must not be read into a
+    group: exactly the definition."""
+    gen = torch.Generator().manual_seed(K * N)
+    W = torch.randn(K, N, generator=gen).to(torch.bfloat16)
+    wide = torch.full((K + 1, N + lead + 3), float("nan"), dtype=torch.bfloat16, device=DEV)
+    wide[:K, lead:N + lead] = W.to(DEV)
+    g = torch.rand(K, generator=gen) + 0.5
+    w4 = fn.fold_weights_w4(wide[:K, lead:N + lead], g.to(DEV), layout=fn.FN_LAYOUT_GLU if glu else fn.FN_LAYOUT_LINEAR,
+                            group=group, zero_points=True)
+    assert np.array_equal(fn.unpack_weights_w4(w4).cpu().double().numpy(), quantise(W, g, group, True))
