@@ -15,14 +15,17 @@ __device__ __forceinline__ double twelve_bits(double s) {
   return __longlong_as_double((long long)(u & ~((1ull << 41) - 1ull)));
 }
 
-// A group's scale and zero point from its extremes.  R(span) below 2^-126 is 0, beyond fp32 NaN; then z = 8.
+// A group's scale and zero point from its extremes, and the quotient -lo / s that z is rounded from (0 where there is
+// none).  R(span) below 2^-126 is 0, beyond fp32 NaN; then z = 8.
 __device__ __forceinline__ double w4_span(double lo, double hi, bool zero_points) {
   return zero_points ? (hi - lo) / 15.0 : fmax(-lo, hi) / 7.0;
 }
-__device__ __forceinline__ void w4_scale_of(double span, double lo, bool bad, bool zero_points, float& s, float& z) {
+__device__ __forceinline__ double w4_scale_of(double span, double lo, bool bad, bool zero_points, float& s, float& z) {
   const double d = twelve_bits(span);
   s = bad || !(d <= 0x1.fffffep127) ? __builtin_nanf("") : d < 0x1p-126 ? 0.0f : (float)d;
-  z = zero_points && s > 0.0f ? (float)fmin(fmax(rint(-lo / d), 0.0), 15.0) : 8.0f;
+  const double at = zero_points && s > 0.0f ? -lo / d : 0.0;
+  z = zero_points && s > 0.0f ? (float)fmin(fmax(rint(at), 0.0), 15.0) : 8.0f;
+  return at;
 }
 
 // A weight view and the position of a lane's 32 values in it: k0 + 32 u + e.
@@ -74,6 +77,8 @@ __device__ __forceinline__ float w4_norm_of(unsigned top) {
 //   the extremes and the span are off by at most 2^-24 of themselves, so the scale is the exact one's unless a
 //   border between twelve-bit values lies that near (one group in 1000: the products that round to the extremes
 //   are taken again in fp64);
+//   the zero point's quotient -lo / s (at most 15 and a bit), by that scale, is off by 2^-24 of itself, less than
+//   2^-19, so it rounds to the right one unless it is that near to a half (then again in fp64);
 //   a quotient (at most 16) is off by 3 * 2^-24 of itself, less than 2^-18, so its nearest whole number is the
 //   right one unless it is that near to a half (one weight in 130000: decided again in fp64).
 // Groups whose largest product is not between 2^-100 and 2^100 are taken in fp64 throughout, but for zeros.
@@ -156,13 +161,13 @@ __global__ __launch_bounds__(WHOLE ? 1024 : 256) void w4_fold_kernel(
     if (j == mine) lo_m = lo, hi_m = hi, any_m = any;
   }
   const double span = w4_span(lo_m, hi_m, zero_points);
-  const float top = fmaxf(-lo_m, hi_m), q0 = zero_points ? lo_m / (float)span : 0.0f;
+  const float top = fmaxf(-lo_m, hi_m);
   float s_m, z_m;
-  w4_scale_of(span, lo_m, false, zero_points, s_m, z_m);
+  const double at_m = w4_scale_of(span, lo_m, false, zero_points, s_m, z_m);
   const bool far_m = any_m != any_m || !(top == 0.0f || (top >= 0x1p-100f && top <= 0x1p100f));
   const bool near_m =
       top > 0.0f && (twelve_bits(span * (1.0 - 0x1p-23)) != twelve_bits(span * (1.0 + 0x1p-23)) ||
-                     fabsf(q0 - rintf(q0)) > 0.5f - 0x1p-12f);  // q0 from the unrounded span: 2^-12 off
+                     fabs(at_m - rint(at_m)) > 0.5 - 0x1p-19);
   if (__any(near_m | far_m)) {
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
