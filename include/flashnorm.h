@@ -445,8 +445,10 @@ size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout, 
 
 /* flashnorm_linear, flashnorm_glu and rowscale_linear with a 4-bit weight.  Sums are fp32.  Few
  * rows, and narrow products of more, multiply the codes unrounded and scale a group's sum; wide
- * products of many rows multiply a weight that is rounded to 11 bits (at most 2^-11 of it, with its scale's rounding).  Which way a call goes
- * depends on M, K, N, the layout, the group and the presence of g alone.
+ * products of many rows multiply a weight that is rounded to 11 bits: with its scale's rounding it
+ * is off by at most 2^-11 of itself and 2^-28 of the largest scale of its column (which counts
+ * where a group's scale is 2^-17 of that or less), and an activation by 2^-39 of its row's largest.
+ * Which way a call goes depends on M, K, N, the layout, the group and the presence of g alone.
  *   a       [M, K] bf16 (fp32: FN_ERR_UNSUPPORTED), any M, K a multiple of 8.
  *   g       optional [K] fp32 norm weight applied at run time, for a weight into which none
  *           is folded.  a[m,k] g[k] enters the product with 11 bits or more (flashnorm_linear_unfolded

@@ -258,7 +258,9 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
 // that puts its largest value into [2^14, 2^15), and a weight is widened to the fp16 of (q - z) r, r its
 // group's scale times a power of two of the column.  Eleven bits hold a bf16 activation exactly and round
 // a weight by 2^-12 at most, an eighth of the output's own rounding in the sums' root mean square, and what
-// lies 2^-29 below a row's largest value or 2^-24 below a column's largest scale fades into the subnormals.
+// lies 2^-29 below a row's largest value or 2^-24 below a column's largest scale fades into the subnormals: their
+// steps of 2^-24 leave an activation off by at most 2^-39 of the row's largest value, and a weight by (|q - z| + 1) 2^-25
+// of the column's power of two, 2^-28 of its largest scale.
 // So the matrix cores sum over all of K: no group of k needs a sum of its own, and no activation statistics
 // are left to the product.
 //
@@ -363,16 +365,17 @@ __global__ __launch_bounds__(T) void w4_rows_kernel(const __bf16* __restrict__ a
   }
 }
 
-// The eight weights of a word as fp16 (q - z) r, in k order.  zero holds 1024 + z twice, r and r16 the
-// group's scale and a sixteenth of it: the odd nibbles are taken where they stand, as 16 q.
-__device__ __forceinline__ f16x8 w4_widen_f16(unsigned w, const W4Bits& k, f16x2 zero, f16x2 zero16, f16x2 r,
-                                               f16x2 r16) {
+// The eight weights of a word as fp16 (q - z) r, in k order.  zero holds 1024 + z twice, zero64 64 + z, r the group's
+// scale.  The odd nibbles are taken where they stand, 1024 + 16 q, whose sixteenth less 64 + z is q - z again, exactly:
+// a sixteenth of r instead would be subnormal, and lose bits, sixteen times sooner than r.
+__device__ __forceinline__ f16x8 w4_widen_f16(unsigned w, const W4Bits& k, f16x2 zero, f16x2 zero64, f16x2 r) {
   auto at = [](unsigned v) { return __builtin_bit_cast(f16x2, v); };
+  const f16x2 sixteenth = {0.0625, 0.0625};
   const unsigned h = w >> 8;
   const f16x2 p0 = (at((w & k.low) | k.bias) - zero) * r;
-  const f16x2 p1 = (at((w & k.high) | k.bias) - zero16) * r16;
+  const f16x2 p1 = __builtin_elementwise_fma(at((w & k.high) | k.bias), sixteenth, -zero64) * r;
   const f16x2 p2 = (at((h & k.low) | k.bias) - zero) * r;
-  const f16x2 p3 = (at((h & k.high) | k.bias) - zero16) * r16;
+  const f16x2 p3 = __builtin_elementwise_fma(at((h & k.high) | k.bias), sixteenth, -zero64) * r;
   return f16x8{p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
 }
 
@@ -501,9 +504,7 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
     auto widen = [&](int u, int c) __attribute__((always_inline)) {
       const f16x2 z1 = NG < 4 ? zero[NG < 4 ? u / GB : 0][c] : zero_of(u / GB, c);
       const f16x2 r1 = NG < 4 ? r[NG < 4 ? u / GB : 0][c] : scale_of(u / GB, c);
-      // 1024 + 16 z = 16 (1024 + z) - 15 * 1024, exactly
-      const f16x2 z16 = (z1 - f16x2{1024, 1024}) * f16x2{16, 16} + f16x2{1024, 1024};
-      wv[u & 1][c] = w4_widen_f16(t.w[c][u], bits, z1, z16, r1, r1 * f16x2{0.0625, 0.0625});
+      wv[u & 1][c] = w4_widen_f16(t.w[c][u], bits, z1, z1 - f16x2{960, 960}, r1);
     };
     auto read = [&](int s) __attribute__((always_inline)) {
       av[s % D] = *reinterpret_cast<const f16x8*>(stage + s % MB * 4096 + (((4 * (s / MB) + lch) ^ lrow) * 16));
