@@ -35,6 +35,12 @@ constexpr int kW4KB = 128;         // k extent of a code fragment
 constexpr float kW4Bias = 128.0f;  // added to every code by its bf16 form
 constexpr unsigned kW4ScaleMask = 0xfffff000u;
 
+// Between a wave's writes to LDS and its lanes' reads of what others of its lanes wrote, and before it writes there again:
+// a wave's accesses to LDS are done in the order in which they are issued, and past this no memory access is moved by the
+// compiler, which otherwise keeps that order only as long as it cannot tell the addresses apart.  No instruction comes of
+// it.
+__device__ __forceinline__ void wave_lds_order() { __builtin_amdgcn_wave_barrier(); }
+
 // Bit of code e (0..7) in its word.
 __device__ __forceinline__ constexpr int w4_bit(int e) { return 4 * (e >> 1) + 16 * (e & 1); }
 

@@ -132,6 +132,7 @@ __global__ __launch_bounds__(WHOLE ? 1024 : 256) void w4_fold_kernel(
 #pragma unroll
     for (int i = 0; i < 2 * RUNS; ++i)
       *reinterpret_cast<u32x4*>(&stage[wave][(i * (64 / RUNS) + lane / RUNS) * 16 + run * EL]) = v[i];
+    wave_lds_order();
   }
   const int mine = c & (NG - 1);
   float p[4][8], low[NG], high[NG], lo_m = 0.0f, hi_m = 0.0f, any_m = 0.0f;

@@ -132,6 +132,7 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
   }
   auto compute_set = [&](const Set& t) __attribute__((always_inline)) {
     if constexpr (STAGED) {
+      wave_lds_order();
 #pragma unroll
       for (int q = 0; q < RG; ++q)
 #pragma unroll
@@ -149,6 +150,7 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
             own[256 * q + at] = t.a[q][j];
           }
         }
+      wave_lds_order();
     }
 #pragma unroll
     for (int j = 0; j < NG; ++j) {
