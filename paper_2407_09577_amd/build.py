@@ -3,13 +3,14 @@
 Every ``csrc/*.hip`` file is compiled for gfx950 only, in parallel, then linked
 into one shared library next to this file.  Packed-fp32 VALU instructions are
 disabled for all device code (the kernels use scalar fp32 arithmetic).
-``csrc/binding.cpp`` (host code, against the installed torch) becomes the extension
-module ``_binding`` beside it.
+``csrc/binding.cpp`` (host code, against the installed torch, with the C++ compiler of
+``$CXX``) becomes the extension module ``_binding`` beside it; the library does not need it.
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
 import glob
+import importlib.util
 import os
 import subprocess
 import sys
@@ -68,24 +69,39 @@ def _link_binding(obj: str) -> None:
     os.replace(tmp, BINDING_PATH)
 
 
-def build(verbose: bool = True) -> str:
-    """Compile every source and link the library and the binding; always rebuilds."""
-    os.makedirs(BUILD_DIR, exist_ok=True)
-    srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
-    workers = min(len(srcs) + 1, max(1, (os.cpu_count() or 4)), 8)
-    with cf.ThreadPoolExecutor(max_workers=workers) as ex:
-        binding = ex.submit(_compile_binding)
-        objs = list(ex.map(_compile, srcs))
-        binding_obj = binding.result()
+def _link_library(objs) -> None:
     tmp = LIB_PATH + f".tmp{os.getpid()}"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", *objs, "-o", tmp]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stderr}")
+    if os.path.exists(BINDING_PATH):
+        os.remove(BINDING_PATH)  # made for the library before this one
     os.replace(tmp, LIB_PATH)
-    _link_binding(binding_obj)
+
+
+def build_binding() -> None:
+    """Compile and link the binding alone, against the library that is there."""
+    os.makedirs(BUILD_DIR, exist_ok=True)
+    _link_binding(_compile_binding())
+
+
+def build(verbose: bool = True, binding: bool = True) -> str:
+    """Compile every source and link the library, then the binding; always rebuilds.  The library needs hipcc alone:
+    where the binding cannot be built the library stands before the error is raised, and where there is no torch (or
+    binding is False) it is all that is built."""
+    os.makedirs(BUILD_DIR, exist_ok=True)
+    srcs = sorted(glob.glob(os.path.join(CSRC, "*.hip")))
+    binding = binding and importlib.util.find_spec("torch") is not None
+    workers = min(len(srcs) + 1, max(1, (os.cpu_count() or 4)), 8)
+    with cf.ThreadPoolExecutor(max_workers=workers) as ex:
+        binding_obj = ex.submit(_compile_binding) if binding else None
+        objs = list(ex.map(_compile, srcs))
+    _link_library(objs)
+    if binding_obj:
+        _link_binding(binding_obj.result())
     if verbose:
-        print(f"built {LIB_PATH} from {len(srcs)} sources", file=sys.stderr)
+        print(f"built {LIB_PATH} from {len(srcs)} sources{'' if binding else ', without the binding'}", file=sys.stderr)
     return LIB_PATH
 
 
