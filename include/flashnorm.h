@@ -458,6 +458,7 @@ size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout, 
  *   workspace  flashnorm_w4_workspace_size bytes, 16-byte aligned, written by the call; one
  *           workspace serves calls that follow each other on a stream (FN_ERR_SIZE where it is
  *           too small, FN_ERR_NULL where it is needed and missing).
+ * Outputs of some 2^40 elements and more are FN_ERR_SIZE.
  * bias, inv_rms, outputs and errors as for the bf16-weight forms; no output may overlap an
  * input or another output (FN_ERR_ALIAS).  A row of a that holds a NaN or an infinity gives NaN.
  * But for the sum of squares, no sum on the way overflows for |a|, |a g| up to 2^100 and |s| up to

@@ -113,10 +113,21 @@ W4Plan w4_plan(int M, int K, int KB, int NP, bool glu, int group, bool gs) {
   return few.us <= many.us ? few.plan : many.plan;
 }
 
+// Rows that go through the kernels together: a launch has fewer than 2^32 threads, up to 1024 per workgroup and, in the
+// many-row kernel's pass over the rows, up to 1024 per row.  0 where one block of rows is too many already.
+static int64_t piece_rows(const W4Plan& plan, int64_t NP) {
+  constexpr int64_t kMost = (int64_t(1) << 22) - 1;
+  const W4Shape& s = plan.many ? kW4Many[plan.shape] : kW4Few[plan.shape];
+  const int64_t rows = kMost / ((NP + s.cols - 1) / s.cols * plan.splits) * s.rows;
+  return plan.many && rows > kMost ? kMost / s.rows * s.rows : rows;
+}
+
 // Workspace of a call: the rows' factors, the fp16 activations and the splits' sums; 0 for the few-row kernel.
 static int64_t factor_bytes(int64_t M) { return round_up(M * 4, 256); }
 int64_t w4_workspace(const W4Plan& plan, int64_t M, int64_t KB, int64_t NP) {
   if (!plan.many) return 0;
+  const int64_t piece = piece_rows(plan, NP);
+  if (M > piece) M = piece;
   return factor_bytes(M) + M * KB * (2 * kW4KB) + (plan.splits > 1 ? plan.splits * M * NP * 4 : 0);
 }
 
@@ -144,13 +155,8 @@ static hipError_t launch_w4_rows(const W4Args& p, _Float16* out, float* factor) 
   return go(w4_rows_kernel<NORM, 1024, 0>, 1024);
 }
 
-hipError_t launch_w4(const W4Args& p) {
+static hipError_t launch_w4_piece(const W4Args& p) {
   const W4Plan& plan = p.plan;
-  const W4Shape& s = plan.many ? kW4Many[plan.shape] : kW4Few[plan.shape];
-  const int64_t groups = (p.M + s.rows - 1) / s.rows, wgs = groups * ((p.NP + s.cols - 1) / s.cols) * plan.splits;
-  // A launch has fewer than 2^32 threads: up to 1024 per workgroup, in the pass over the rows too.
-  if (wgs * 1024 >= (int64_t(1) << 32) || (plan.many && (int64_t)p.M * 1024 >= (int64_t(1) << 32)))
-    return hipErrorInvalidConfiguration;
   if (!plan.many) {
     switch (p.epi) {
       case EPI_RMS: return launch_w4_few<EPI_RMS>(p, plan.shape);
@@ -165,18 +171,38 @@ hipError_t launch_w4(const W4Args& p) {
   float* partial = reinterpret_cast<float*>(ws + factor_bytes(p.M) + (int64_t)p.M * p.KB * (2 * kW4KB));
   const hipError_t e = p.epi == EPI_ROWSCALE ? launch_w4_rows<false>(p, act, factor) : launch_w4_rows<true>(p, act, factor);
   if (e != hipSuccess) return e;
+  const int rows = kW4Many[plan.shape].rows, groups = (p.M + rows - 1) / rows;
   // Row groups that share a column tile's codes in an XCD's L2: all of them where their activations fit it (4 MB)
   // beside each other, else pairs, whose activations it holds while the tiles go by.  All / pairs: 333 x 4096 -> 12288
   // 58.2 / 61.0 us, 2048 x 11008 -> 4096 187 / 177; panels of four and eight are no better there.
-  const int panel = (int64_t)p.M * p.KB * (2 * kW4KB) <= (4 << 20) ? (int)groups : 2;
+  const int panel = (int64_t)p.M * p.KB * (2 * kW4KB) <= (4 << 20) ? groups : 2;
   const W4Gemm q{act, p.M, p.KB * kW4KB, p.codes, p.scales, p.norms, p.NP, p.KB, p.ncols, factor, p.ep.bias, p.y, p.ldy,
-                 (int)groups, panel, plan.splits, plan.kb_per_split, partial};
+                 groups, panel, plan.splits, plan.kb_per_split, partial};
   switch (p.epi) {
     case EPI_RMS: return launch_w4_many<EPI_RMS>(q, p.group, plan.shape, p.stream);
     case EPI_GLU: return launch_w4_many<EPI_GLU>(q, p.group, plan.shape, p.stream);
     case EPI_ROWSCALE: return launch_w4_many<EPI_ROWSCALE>(q, p.group, plan.shape, p.stream);
   }
   return hipErrorInvalidValue;
+}
+
+// More rows than a launch takes go in pieces, one after the other on the stream and in the same workspace.
+hipError_t launch_w4(const W4Args& p) {
+  constexpr int64_t kPieces = 1024;  // beyond, the output has some 2^40 elements
+  const int64_t piece = piece_rows(p.plan, p.NP);
+  if (p.M <= piece) return launch_w4_piece(p);
+  if (p.M > piece * kPieces) return hipErrorInvalidConfiguration;
+  for (int64_t m = 0; m < p.M; m += piece) {
+    W4Args q = p;
+    q.M = (int)(p.M - m < piece ? p.M - m : piece);
+    q.a += m * p.lda;
+    q.y += m * p.ldy;
+    if (q.ep.inv_rms) q.ep.inv_rms += m;
+    if (q.ep.row_scale) q.ep.row_scale += m;
+    const hipError_t e = launch_w4_piece(q);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace fn
