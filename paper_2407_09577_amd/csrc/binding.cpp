@@ -13,6 +13,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <stdexcept>
 #include <string>
 
@@ -130,6 +131,13 @@ Tensor new_matrix(const Call& c, int64_t rows, int64_t cols) {
   const int64_t ld = (cols + c.per - 1) / c.per * c.per;
   const Tensor t = new_tensor(c, {rows, ld}, c.type);
   return ld == cols ? t : t.narrow(1, 0, cols);
+}
+
+// The caller's tensors that a call has written count as changed for autograd, which refuses a backward pass through
+// values it kept of them (inference tensors have no count).
+void written(std::initializer_list<const Tensor*> given) {
+  for (const Tensor* t : given)
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
 }
 
 // The caller's workspace, checked, or a new one.
@@ -267,6 +275,7 @@ PyObject* w4_product(PyObject*, PyObject* const* v, Py_ssize_t n) {
       s = rowscale_linear_w4(A.p, M, K, A.ld, c.code, data.data_ptr(), N, group, row_scale, Y.p, Y.ld, c.code, address(ws),
                              need, stream_of(c));
     if (s) return PyLong_FromLong(s);
+    written({out, tensor_or_none(v[11]), need ? tensor_or_none(v[13]) : nullptr});
     return out ? again(v[10]) : wrap(made);
   });
 }
@@ -301,6 +310,7 @@ PyObject* block_residual(PyObject*, PyObject* const* v, Py_ssize_t n) {
                                            real(v[6]), real(v[7]), g_pre, real(v[9]), O.p, O.ld, NO.p, NO.ld, inv_rms,
                                            stream_of(c));
     if (s) return PyLong_FromLong(s);
+    written({out, normed, tensor_or_none(v[12])});
     PyObject* first = out ? again(v[10]) : wrap(made);
     PyObject* second = normed ? again(v[11]) : wrap(made_n);
     PyObject* both = first && second ? PyTuple_Pack(2, first, second) : nullptr;
@@ -338,6 +348,7 @@ PyObject* block_residual_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
         real(v[9]), g_pre, real(v[11]), DX.p, DX.ld, DH.p, DH.ld, DG.p, DG.ld, static_cast<float*>(address(dpost)),
         static_cast<float*>(address(dpre)), address(ws), need, stream_of(c));
     if (s) return PyLong_FromLong(s);
+    written({need ? tensor_or_none(v[12]) : nullptr});
     PyObject* parts[] = {wrap(dx), wrap(dh), wrap(dgate), wrap(dpost), wrap(dpre)};
     bool whole = true;
     for (PyObject* p : parts) whole = whole && p;

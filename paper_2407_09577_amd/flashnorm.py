@@ -540,7 +540,8 @@ def baseline_layernorm_linear(a, g, beta, W_packed, N, eps, x_ws=None, out=None,
 
 # The 4-bit weights and the block residual run on the GPU of their tensors, whatever the current one
 # is, and what they allocate belongs to the stream that works on it: a call for another GPU or stream
-# makes that one current and starts again.
+# makes that one current and starts again.  autograd records none of these calls, but counts what they
+# write into the caller's tensors as changed.
 def _current_device():
     return _raw_device() if _raw_device else torch.cuda.current_device()
 
@@ -684,7 +685,9 @@ def flashnorm_block_residual(x: torch.Tensor, h: torch.Tensor, g_post=None, eps_
                              rows_per_gate: int = 1, res_scale: float = 1.0, branch_scale: float = 1.0, g_pre=None,
                              eps_pre: float = 0.0, out=None, normed=None, inv_rms=None, stream=None):
     """out = res_scale h + branch_scale gate RMSNorm(x; g_post), normed = RMSNorm(out; g_pre).  Returns
-    (out, normed); normed is None without g_pre.  out may be h, normed may be x."""
+    (out, normed); normed is None without g_pre.  out may be h, normed may be x.  autograd does not record the
+    call: its outputs carry no gradient, whatever its inputs require; flashnorm_block_residual_bwd gives the
+    gradients, from h as it was before the call."""
     return _call("flashnorm_block_residual", "block_residual", x, stream, x, h, g_post, eps_post, gate, rows_per_gate,
                  res_scale, branch_scale, g_pre, eps_pre, out, normed, inv_rms)
 
