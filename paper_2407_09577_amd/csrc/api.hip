@@ -154,8 +154,7 @@ int fold_weights(const void* W, int64_t stride_k, int64_t stride_n, int w_dtype,
   if (layout == FN_LAYOUT_GLU && (colsum || c_star)) return FN_ERR_UNSUPPORTED;
   if (!aligned16(W_star) || (reinterpret_cast<uintptr_t>(W) % elem_size(w_dtype))) return FN_ERR_ALIGN;
   const int64_t wsb = (int64_t)fold_weights_size(K, N, layout, ws_dtype);
-  // Bytes spanned by the strided view (the largest element offset is below 2^62).
-  const int64_t wext = ((K - 1) * stride_k + (N - 1) * stride_n + 1) * elem_size(w_dtype);
+  const int64_t wext = view_bytes(K, N, stride_k, stride_n, w_dtype);
   if (overlaps(W_star, wsb, W, wext)) return FN_ERR_ALIAS;
   fn::FoldArgs p{W, stride_k, stride_n, w_dtype, g, beta, K, N, layout == FN_LAYOUT_GLU, W_star, ws_dtype,
                  colsum, c_star, (hipStream_t)stream};

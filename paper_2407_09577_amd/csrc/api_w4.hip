@@ -122,7 +122,7 @@ int fold_weights_w4(const void* W, int64_t stride_k, int64_t stride_n, int w_dty
   if (!W || !W4) return FN_ERR_NULL;
   if (!aligned16(W4) || reinterpret_cast<uintptr_t>(W) % elem_size(w_dtype)) return FN_ERR_ALIGN;
   const int64_t wb = fn::w4_bytes(K, N, layout == FN_LAYOUT_GLU, group);
-  const int64_t wext = ((K - 1) * stride_k + (N - 1) * stride_n + 1) * elem_size(w_dtype);
+  const int64_t wext = view_bytes(K, N, stride_k, stride_n, w_dtype);
   if (overlaps(W4, wb, W, wext) || (g && overlaps(W4, wb, g, K * 4))) return FN_ERR_ALIAS;
   fn::W4FoldArgs p{W, stride_k, stride_n, w_dtype, g, K, N, layout == FN_LAYOUT_GLU, group, zero_points != 0, W4,
                    (hipStream_t)stream};

@@ -38,6 +38,12 @@ inline int64_t extent_bytes(int64_t rows, int64_t cols, int64_t ld, int dtype) {
   return rows > 0 ? ((rows - 1) * ld + cols) * elem_size(dtype) : 0;
 }
 
+// Bytes spanned by a strided view.  The largest element offset is below 2^62, its bytes may pass 2^63: they are counted
+// without a sign, as overlaps() does.
+inline int64_t view_bytes(int64_t K, int64_t N, int64_t stride_k, int64_t stride_n, int dtype) {
+  return (int64_t)((uint64_t)((K - 1) * stride_k + (N - 1) * stride_n + 1) * (uint64_t)elem_size(dtype));
+}
+
 // Common checks of an activation-like operand [M, K] with leading dimension ld.
 inline int check_matrix(const void* p, int64_t M, int64_t K, int64_t ld, int dtype, bool required) {
   if (M < 0 || K <= 0 || M > kMaxRows) return FN_ERR_SHAPE;
