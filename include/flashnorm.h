@@ -424,7 +424,8 @@ int fold_weights_w4(const void* W, int64_t stride_k, int64_t stride_n, int w_dty
 
 /* Pack a weight that is in 4 bits already (a checkpoint's), unchanged.
  *   codes   [K, N] one code per byte, row stride ldc; the low 4 bits count.
- *   scales  [ceil(K / group), N] fp32, row stride lds, rounded to 12 significant bits.
+ *   scales  [ceil(K / group), N] fp32, row stride lds, rounded to 12 significant bits.  A column with an
+ *           infinite or NaN scale gives infinite or NaN outputs.
  *   zeros   [ceil(K / group), N] zero points, row stride ldz, of which the low 6
  *           bits count (0..63); NULL for 8 throughout.
  * For FN_LAYOUT_GLU the columns are [gate | up].  No norm weight can be folded into codes:
@@ -444,7 +445,8 @@ int unpack_weights_w4(const void* W4, int64_t K, int64_t N, int layout, int grou
 size_t flashnorm_w4_workspace_size(int64_t M, int64_t K, int64_t N, int layout, int group);
 
 /* flashnorm_linear, flashnorm_glu and rowscale_linear with a 4-bit weight.  Sums are fp32.  Few
- * rows, and narrow products of more, multiply the codes unrounded and scale a group's sum; wide
+ * rows, and narrow products of more, multiply the codes unrounded and scale a group's sum, which is
+ * off by at most 2^-10 of the group's |s| sum |a| (some 2^-18 of its sum |a w| as a rule); wide
  * products of many rows multiply a weight that is rounded to 11 bits: with its scale's rounding it
  * is off by at most 2^-11 of itself and 2^-28 of the largest scale of its column (which counts
  * where a group's scale is 2^-17 of that or less), and an activation by 2^-39 of its row's largest.

@@ -20,7 +20,9 @@
 // activations takes the 128 + z off again:
 //   sum_k a (q - z) s = s (sum_k a (128 + q) - (128 + z) sum_k a).
 // No weight is rounded: the bf16 products are exact, the sums are fp32.  The offset costs last bits of
-// the sums, 2^-18 of sum |a w|.
+// them: partial sums below 143 sum |a| and, with z up to 63, 191 sum |a| leave a group off by at most 2^-10
+// of |s| sum |a|, whatever its codes (a group that stands for zeros has that residue too).  For codes
+// spread around z it is some 2^-18 of sum |a w|.
 // Many rows: OR'ed with 0x6400 a half is the fp16 1024 + q; less 1024 + z, times the scale as fp16, it is
 // the weight in eleven bits (w4_kernels.h).
 // The products run with the activations as the matrix cores' first operand, so a lane's four results
