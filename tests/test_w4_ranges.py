@@ -54,3 +54,28 @@ def test_small_scales_beside_large_ones(fn, exponent, alike, group):
     tol = 2.0 ** -8 * ref.abs() + 2.0 ** -11 * A + 16 * 2.0 ** -24 * A + 2.0 ** -30 * a.double().sum(1, keepdim=True) * top
     over = (y - ref).abs() / tol
     assert torch.isfinite(y).all() and over.max() <= 1, float(over.max())
+
+
+@pytest.mark.parametrize("M", [3, 20, 300])
+def test_rows_far_from_one(fn, M):
+    """Rows of 2^-116 to 2^100, their subnormal bf16 values among them, through a weight of about one: 2^-13 of
+    8 sum |a s| and 1.5 * 2^-11 of sum |a w| as in test_w4.py, and half a step of the output's subnormals."""
+    K, N, group = 1024, 5000 if M == 300 else 200, 64
+    assert plan(M, K, N, False, group, False).many == (M == 300)
+    gen = torch.Generator(DEV).manual_seed(M)
+    codes = torch.randint(0, 16, (K, N), generator=gen, device=DEV, dtype=torch.uint8)
+    scales = (torch.rand(K // group, N, generator=gen, device=DEV) + 0.5).to(torch.bfloat16)
+    e = torch.tensor([-116, -100, -60, 0, 60, 100], device=DEV)[torch.arange(M, device=DEV) % 6]
+    a = (torch.randn(M, K, generator=gen, device=DEV).double() * torch.exp2(e.double())[:, None]).to(torch.bfloat16)
+    scale = torch.rand(M, generator=gen, device=DEV) + 0.5
+    w4 = fn.pack_weights_w4(codes, scales, group=group)
+    s = scales.double().repeat_interleave(group, 0)
+    W = (codes.double() - 8.0) * s
+    for rs in (None, scale):
+        y = fn.rowscale_linear_w4(a, w4, row_scale=rs)
+        f = torch.ones(M, 1, dtype=torch.float64, device=DEV) if rs is None else rs.double()[:, None]
+        x = a.double()
+        ref = (x @ W) * f
+        tol = 2.0 ** -8 * ref.abs() + (2.0 ** -13 * (x.abs() @ (8.0 * s)) + 1.5 * 2.0 ** -11 * (x.abs() @ W.abs())) * f + 2.0 ** -134
+        over = (y.double() - ref).abs() / tol
+        assert torch.isfinite(y).all() and over.max() <= 1, float(over.max())
