@@ -267,15 +267,16 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
 // are left to the product.
 //
 // One workgroup per row: the row's squares and largest value, then its fp16 form, [KB * 128] with zeros
-// past K, and the factor that the outputs take: (1 / RMSe, or the given row scale) / the power of two.
+// past K, and the factor that the outputs take: 1 / the power of two, and 1 / RMSe times that.  A given row scale
+// comes after it: the product of the two could leave fp32 where neither does.
 // With g the values are a g, rounded to fp16.  A row that holds a NaN or an infinity gets a NaN factor.
 // T threads hold up to H pieces of 16 bytes each; H = 0: the row is read twice.  Bound by its launch and one trip to
 // memory: 333 x 4096 5.2 us, 2048 x 4096 10.5 us.
 template <bool NORM, int T, int H>
 __global__ __launch_bounds__(T) void w4_rows_kernel(const __bf16* __restrict__ a, int K, int lda,
-                                                    const float* __restrict__ g, const float* __restrict__ row_scale,
-                                                    float eps, float inv_k, int KP, _Float16* __restrict__ out,
-                                                    float* __restrict__ factor, float* __restrict__ inv_rms) {
+                                                    const float* __restrict__ g, float eps, float inv_k, int KP,
+                                                    _Float16* __restrict__ out, float* __restrict__ factor,
+                                                    float* __restrict__ inv_rms) {
   __shared__ float red[T / 64];
   __shared__ unsigned red_top[T / 64];
   const int64_t m = blockIdx.x;
@@ -348,8 +349,6 @@ __global__ __launch_bounds__(T) void w4_rows_kernel(const __bf16* __restrict__ a
     if constexpr (NORM) {
       s = rsqrtf(fmaf(ss, inv_k, eps));
       if (inv_rms) inv_rms[m] = s;
-    } else if (row_scale) {
-      s = row_scale[m];
     }
     factor[m] = ex == 255u ? __builtin_nanf("") : s * (1.0f / f);
   }
@@ -398,7 +397,8 @@ struct W4Gemm {
   const unsigned* scales;
   const float* col_norm;  // [NP] the columns' powers of two
   int NP, KB, ncols;
-  const float* factor;  // [M]
+  const float* factor;     // [M]
+  const float* row_scale;  // EPI_ROWSCALE: optional [M]
   const float* bias;
   __bf16* y;
   int ldy;
@@ -406,6 +406,18 @@ struct W4Gemm {
   int splits, kb_per_split;
   float* partial;  // [splits][M][NP]
 };
+
+// One output of the many-row kernel from its sums, the row's factor and the columns' 1 / norm.
+template <int EPI>
+__device__ __forceinline__ float w4_many_value(float v, float u, float n0, float n1, float factor, float scale, float bias) {
+  if constexpr (EPI == EPI_ROWSCALE) return v * n0 * factor * scale;
+  else return w4_value<EPI>(v * n0, u * n1, factor, bias);
+}
+
+template <int EPI>
+__device__ __forceinline__ float w4_given_scale(const W4Gemm& p, int64_t m) {
+  return EPI == EPI_ROWSCALE && p.row_scale ? p.row_scale[m] : 1.0f;
+}
 
 template <int MB, int NCB, int WM, int WN, int KS, int NST, int GB, int EPI>
 __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p) {
@@ -607,9 +619,12 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
   for (int t = 0; t < MB; ++t) {
     if (t % KS != kg) continue;
     const int row = (wm * MB + t) * 16 + lch * 4;
-    float s[4];
+    float s[4], given[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) s[r] = row + r < rows ? p.factor[m0 + row + r] : 0.0f;
+    for (int r = 0; r < 4; ++r) {
+      s[r] = row + r < rows ? p.factor[m0 + row + r] : 0.0f;
+      given[r] = row + r < rows ? w4_given_scale<EPI>(p, m0 + row + r) : 0.0f;
+    }
 #pragma unroll
     for (int c = 0; c < NCB; c += STEP) {
       const int col = (wn * NCB + c) / STEP * 16 + lrow;
@@ -617,7 +632,8 @@ __global__ __launch_bounds__(64 * WM * WN * KS, 2) void w4_gemm_kernel(W4Gemm p)
       const float f0 = 1.0f / norm[c], f1 = 1.0f / norm[c + STEP - 1];
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        out[(row + r) * PITCH + col] = (__bf16)w4_value<EPI>(acc[t][c][r] * f0, acc[t][c + STEP - 1][r] * f1, s[r], bias);
+        out[(row + r) * PITCH + col] =
+            (__bf16)w4_many_value<EPI>(acc[t][c][r], acc[t][c + STEP - 1][r], f0, f1, s[r], given[r], bias);
     }
   }
   __syncthreads();
@@ -660,7 +676,7 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Gemm p) {
 #pragma unroll
     for (int s = 0; s < 8; ++s) v += a[s], u += b[s];
   }
-  const float f = p.factor[m];
+  const float f = p.factor[m], given = w4_given_scale<EPI>(p, m);
   const f32x4 n0 = *reinterpret_cast<const f32x4*>(p.col_norm + c);
   f32x4 n1 = n0;
   if constexpr (STEP == 2) n1 = *reinterpret_cast<const f32x4*>(p.col_norm + c + 16);
@@ -668,7 +684,7 @@ __global__ __launch_bounds__(256) void w4_join_kernel(W4Gemm p) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     const float bias = EPI == EPI_RMS && p.bias && n + e < p.ncols ? p.bias[n + e] : 0.0f;
-    o[e] = w4_value<EPI>(v[e] * (1.0f / n0[e]), u[e] * (1.0f / n1[e]), f, bias);
+    o[e] = w4_many_value<EPI>(v[e], u[e], 1.0f / n0[e], 1.0f / n1[e], f, given, bias);
   }
   __bf16* dst = p.y + m * p.ldy + n;
   if (n + 4 <= p.ncols) {

@@ -145,8 +145,8 @@ template <bool NORM>
 static hipError_t launch_w4_rows(const W4Args& p, _Float16* out, float* factor) {
   const int KP = p.KB * kW4KB;
   auto go = [&](auto kernel, int threads) {
-    hipLaunchKernelGGL(kernel, dim3(p.M), dim3(threads), 0, p.stream, p.a, p.K, p.lda, p.ep.g_rt, p.ep.row_scale, p.ep.eps,
-                       p.ep.inv_k, KP, out, factor, p.ep.inv_rms);
+    hipLaunchKernelGGL(kernel, dim3(p.M), dim3(threads), 0, p.stream, p.a, p.K, p.lda, p.ep.g_rt, p.ep.eps, p.ep.inv_k,
+                       KP, out, factor, p.ep.inv_rms);
     return hipGetLastError();
   };
   // More threads for long rows where rows alone do not fill the chip (64 x 11008: the call 25.1 -> 22.5 us).
@@ -176,8 +176,8 @@ static hipError_t launch_w4_piece(const W4Args& p) {
   // beside each other, else pairs, whose activations it holds while the tiles go by.  All / pairs: 333 x 4096 -> 12288
   // 58.2 / 61.0 us, 2048 x 11008 -> 4096 187 / 177; panels of four and eight are no better there.
   const int panel = (int64_t)p.M * p.KB * (2 * kW4KB) <= (4 << 20) ? groups : 2;
-  const W4Gemm q{act, p.M, p.KB * kW4KB, p.codes, p.scales, p.norms, p.NP, p.KB, p.ncols, factor, p.ep.bias, p.y, p.ldy,
-                 groups, panel, plan.splits, plan.kb_per_split, partial};
+  const W4Gemm q{act, p.M, p.KB * kW4KB, p.codes, p.scales, p.norms, p.NP, p.KB, p.ncols, factor, p.ep.row_scale,
+                 p.ep.bias, p.y, p.ldy, groups, panel, plan.splits, plan.kb_per_split, partial};
   switch (p.epi) {
     case EPI_RMS: return launch_w4_many<EPI_RMS>(q, p.group, plan.shape, p.stream);
     case EPI_GLU: return launch_w4_many<EPI_GLU>(q, p.group, plan.shape, p.stream);

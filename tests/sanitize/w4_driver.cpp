@@ -71,6 +71,7 @@ static void check_products(int64_t M, int64_t K, int64_t N, int group, int kind,
                               (const char*)(p.partial + (int64_t)p.splits * p.M * p.NP) <= ws + need));
       CHECK(pass < stub_launches.size() && stub_launches[pass].grid.x == (unsigned)p.M);  // a workgroup for each row
       ++pass;
+      CHECK(p.row_scale == (kind == 2 ? PF(R) + m : nullptr));
     } else {
       CHECK(p.a == (const char*)P(A) + m * K * 2);
       CHECK(kind == 2 ? p.row_scale == PF(R) + m : kind != 0 || p.inv_rms == PF(R) + m);

@@ -18,7 +18,7 @@ namespace fn {
   }                                                                                                          \
   template <>                                                                                                \
   hipError_t launch_w4_many<EPI>(const W4Gemm& q, int, int shape, hipStream_t) {                             \
-    stub_products.push_back(stub_product{true, EPI, shape, q.M, q.NP, q.KB, q.splits, q.a, q.y, nullptr, nullptr, q.factor, \
+    stub_products.push_back(stub_product{true, EPI, shape, q.M, q.NP, q.KB, q.splits, q.a, q.y, nullptr, q.row_scale, q.factor, \
                                          q.partial, q.groups});                                              \
     return hipSuccess;                                                                                       \
   }

@@ -79,3 +79,23 @@ def test_rows_far_from_one(fn, M):
         tol = 2.0 ** -8 * ref.abs() + (2.0 ** -13 * (x.abs() @ (8.0 * s)) + 1.5 * 2.0 ** -11 * (x.abs() @ W.abs())) * f + 2.0 ** -134
         over = (y.double() - ref).abs() / tol
         assert torch.isfinite(y).all() and over.max() <= 1, float(over.max())
+
+
+@pytest.mark.parametrize("M", [3, 20, 300])
+@pytest.mark.parametrize("rows,scales_at,row_scale", [(100, -80, 50), (-60, 80, -60), (90, 0, -100), (-100, 60, 100), (0, -70, 120)])
+def test_row_scales_far_from_one(fn, rows, scales_at, row_scale, M):
+    """A row's values, the weight's scales and the row's scale far from one, and the output near it."""
+    K, N, group = 1024, 5000 if M == 300 else 200, 32
+    gen = torch.Generator(DEV).manual_seed(M)
+    codes = torch.randint(0, 16, (K, N), generator=gen, device=DEV, dtype=torch.uint8)
+    scales = ((torch.rand(K // group, N, generator=gen, device=DEV) + 0.5) * 2.0 ** scales_at).to(torch.bfloat16)
+    a = (torch.randn(M, K, generator=gen, device=DEV).clamp(-1, 1) * 2.0 ** rows).to(torch.bfloat16)
+    scale = (torch.rand(M, generator=gen, device=DEV) + 0.5) * 2.0 ** row_scale
+    w4 = fn.pack_weights_w4(codes, scales, group=group)
+    y = fn.rowscale_linear_w4(a, w4, row_scale=scale)
+    s = scales.double().repeat_interleave(group, 0)
+    W, x, f = (codes.double() - 8.0) * s, a.double(), scale.double()[:, None]
+    ref = (x @ W) * f
+    tol = 2.0 ** -8 * ref.abs() + (2.0 ** -13 * (x.abs() @ (8.0 * s)) + 1.5 * 2.0 ** -11 * (x.abs() @ W.abs())) * f
+    over = (y.double() - ref).abs() / tol
+    assert torch.isfinite(y).all() and over.max() <= 1, float(over.max())
