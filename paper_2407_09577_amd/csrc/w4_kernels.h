@@ -45,9 +45,9 @@ __device__ __forceinline__ void split_ag(const bf16x8& a, const f32x4& g0, const
 // (4096 -> 6144 with one column block a wave: 11.9 -> 9.1 us) and only adds a wait to one of a row or two
 // (two blocks: 6.6 -> 7.6).
 // Kernel times: 1 x 4096 -> 6144 6.8 us, 16 x 4096 -> 22016 GLU 13.8 us for 50 MB, beside 3.1 us of a kernel that does
-// nothing: the stream itself runs at 3.7 to 4.7 TB/s.  64 x 11008 -> 4096 (17.7 us a call) is bound by the widening,
-// once for each 16 rows, and its waits; the matrix cores are busy for an eighth of it.  Loads two blocks ahead gained 5%
-// at K = 11008 and cost as much at 4096.
+// nothing: the stream itself runs at 3.7 to 4.7 TB/s.  64 x 11008 -> 4096 (17.6 to 20.4 us a call on different boxes)
+// widens every code once for each 16 rows and waits in between: vector instructions issue for a third of the time, the
+// matrix cores are busy for an eighth.  Loads two blocks ahead gained 5% at K = 11008 and cost as much at 4096.
 template <int NCB, int KS, int RG, int GB, int EPI, bool GS, bool STAGED>
 __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restrict__ a, int M, int K, int lda,
                                                          const void* __restrict__ codes,
@@ -269,7 +269,9 @@ __global__ __launch_bounds__(64 * KS) void w4_few_kernel(const __bf16* __restric
 // One workgroup per row: the row's squares and largest value, then its fp16 form, [KB * 128] with zeros
 // past K, and the factor that the outputs take: 1 / the power of two, and 1 / RMSe times that.  A given row scale
 // comes after it: the product of the two could leave fp32 where neither does.
-// With g the values are a g, rounded to fp16.  A row that holds a NaN or an infinity gets a NaN factor.
+// With g the values are a g, rounded to fp16, 2^-12 of each at most: an error in the outputs of a twelfth of their own
+// rounding (root mean square), where the few-row kernel's two halves would double the products.
+// A row that holds a NaN or an infinity gets a NaN factor.
 // T threads hold up to H pieces of 16 bytes each; H = 0: the row is read twice.  Bound by its launch and one trip to
 // memory: 333 x 4096 5.2 us, 2048 x 4096 10.5 us.
 template <bool NORM, int T, int H>
@@ -386,9 +388,10 @@ __device__ __forceinline__ f16x8 w4_widen_f16(unsigned w, const W4Bits& k, f16x2
 // ring of NST stages, NST - 1 sets ahead: 16 lanes bring one row's 256 bytes, 16-byte piece j of row r at
 // position j ^ (r % 16), so that the sixteen rows of an operand read lie in different banks.
 // With several `splits` of K each workgroup writes its fp32 sums and w4_join_kernel finishes them.
-// Bound by the matrix cores where there are enough workgroups, else by the waits in one set: 2048 x 4096 -> 22016 GLU
-// 321 us (337 on another box), 1.10 to 1.15 PFLOP/s with the matrix cores busy for half of the time; a set of 128 k takes a workgroup that is alone
-// on its compute unit 2600 cycles, 1024 of them matrix-core operations.  Weights through LDS as well, a third stage,
+// 2048 x 4096 -> 22016 GLU takes 316 to 337 us on different boxes, 1.10 to 1.17 PFLOP/s: the matrix cores are busy for
+// half of the time, and the vector instructions that widen issue for a third.  With fewer workgroups it is the waits in
+// one set that count: a set of 128 k takes a workgroup that is alone on its compute unit 2600 cycles, 1024 of them
+// matrix-core operations.  Weights through LDS as well, a third stage,
 // operands read six or eight steps ahead and widening spread over the steps, into the next set's first, did not help.
 struct W4Gemm {
   const _Float16* a;  // [M][KP]

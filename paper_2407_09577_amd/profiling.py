@@ -4,7 +4,8 @@ A summary records, for one kernel and workload: the commands that produced it,
 the kernel's average duration from ``--kernel-trace --stats`` (over all its dispatches,
 and over the last ``--timed-steps`` ones, the bench's timed region), the FETCH_SIZE and
 WRITE_SIZE counters per dispatch (KiB) scaled by the factors a plain device copy
-of known size yields on the same machine, the matrix-core busy fraction, and a
+of known size yields on the same machine, the matrix-core busy fraction (and, where it was
+taken, the share of the time in which vector instructions issue), and a
 SHA-256 of the kernel's source file and the shared headers.  bench.py reports the
 measured HBM traffic only while that hash still matches the sources.
 
@@ -126,6 +127,12 @@ def summarize(a) -> str:
         conflict, _ = counter_mean(a.lds, a.kernel, "SQ_LDS_BANK_CONFLICT")
         lines.insert(-1, f"lds_bank_conflict_fraction: {conflict / active if active else 0.0:.4f}  "
                          f"(SQ_LDS_BANK_CONFLICT / SQ_LDS_IDX_ACTIVE)")
+    if a.valu:
+        counts = [counter_mean(a.valu, a.kernel, c)[0] for c in ("SQ_INSTS_VALU", "SQ_INSTS_MFMA", "GRBM_GUI_ACTIVE")]
+        # A vector instruction of 64 lanes takes its SIMD four cycles; matrix-core instructions are counted in both.
+        share = (counts[0] - counts[1]) * 4 / (counts[2] / a.xcds * a.simds)
+        lines.insert(-1, f"valu_issue_fraction: {share:.4f}  (4 (SQ_INSTS_VALU - SQ_INSTS_MFMA) / "
+                         f"(GRBM_GUI_ACTIVE/{a.xcds} x {a.simds} SIMDs))")
     return "\n".join(lines) + "\n"
 
 
@@ -154,6 +161,7 @@ def main():
         p.add_argument(f"--{k}", required=True)
     p.add_argument("--trace", default=None, help="--kernel-trace --stats output of the same command")
     p.add_argument("--lds", default=None, help="--pmc SQ_LDS_IDX_ACTIVE SQ_LDS_BANK_CONFLICT output")
+    p.add_argument("--valu", default=None, help="--pmc SQ_INSTS_VALU SQ_INSTS_MFMA GRBM_GUI_ACTIVE output")
     p.add_argument("--timed-what", default="bench.py's last timed graph replay")
     p.add_argument("--copy-bytes", type=int, required=True)
     p.add_argument("--timed-steps", type=int, default=100, help="bench.py --steps of the traced command")
