@@ -45,7 +45,7 @@ __device__ __forceinline__ void split_ag(const bf16x8& a, const f32x4& g0, const
 // (4096 -> 6144 with one column block a wave: 11.9 -> 9.1 us) and only adds a wait to one of a row or two
 // (two blocks: 6.6 -> 7.6).
 // Kernel times: 1 x 4096 -> 6144 6.8 us, 16 x 4096 -> 22016 GLU 13.8 us for 50 MB, beside 3.1 us of a kernel that does
-// nothing: the stream itself runs at 3.7 to 4.7 TB/s.  64 x 11008 -> 4096 (17.6 to 20.4 us a call on different boxes)
+// nothing: the stream itself runs at 3.7 to 4.7 TB/s.  64 x 11008 -> 4096 (17.7 us a call, 20 to 22 traced one by one)
 // widens every code once for each 16 rows and waits in between: vector instructions issue for a third of the time, the
 // matrix cores are busy for an eighth.  Loads two blocks ahead gained 5% at K = 11008 and cost as much at 4096.
 template <int NCB, int KS, int RG, int GB, int EPI, bool GS, bool STAGED>
