@@ -425,7 +425,7 @@ int fold_weights_w4(const void* W, int64_t stride_k, int64_t stride_n, int w_dty
 /* Pack a weight that is in 4 bits already (a checkpoint's), unchanged.
  *   codes   [K, N] one code per byte, row stride ldc; the low 4 bits count.
  *   scales  [ceil(K / group), N] fp32, row stride lds, rounded to 12 significant bits.  A column with an
- *           infinite or NaN scale gives infinite or NaN outputs.
+ *           infinite or NaN scale gives infinite or NaN sums.
  *   zeros   [ceil(K / group), N] zero points, row stride ldz, of which the low 6
  *           bits count (0..63); NULL for 8 throughout.
  * For FN_LAYOUT_GLU the columns are [gate | up].  No norm weight can be folded into codes:

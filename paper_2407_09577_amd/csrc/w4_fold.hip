@@ -84,7 +84,7 @@ __device__ __forceinline__ float w4_norm_of(unsigned top) {
 // Groups whose largest product is not between 2^-100 and 2^100 are taken in fp64 throughout, but for zeros.
 // A wave loads its fragment, waits and computes, 22 vector operations a weight, so neither memory nor the vector units
 // are busy for more than six tenths of the time.  4096 x 22016 bf16 from [N, K]: 114 us with fp64 quotients throughout,
-// 65 to 90 us so (on different boxes), for 228 MB.
+// 65 to 90 us so (on different cards), for 228 MB.
 // A workgroup takes cw column and kw k blocks.  Of the four lanes of a column each makes the scale of one group, if
 // there are as many: made by each lane in turn, four groups' fp64 took 3 us of a small fold and a fifth of a large
 // one (4096 x 22016, groups of 32: 91 us a call, 71 so).  WHOLE: kw is all of K, so the workgroup sees whole columns

@@ -388,7 +388,7 @@ __device__ __forceinline__ f16x8 w4_widen_f16(unsigned w, const W4Bits& k, f16x2
 // ring of NST stages, NST - 1 sets ahead: 16 lanes bring one row's 256 bytes, 16-byte piece j of row r at
 // position j ^ (r % 16), so that the sixteen rows of an operand read lie in different banks.
 // With several `splits` of K each workgroup writes its fp32 sums and w4_join_kernel finishes them.
-// 2048 x 4096 -> 22016 GLU takes 316 to 337 us on different boxes, 1.10 to 1.17 PFLOP/s: the matrix cores are busy for
+// 2048 x 4096 -> 22016 GLU takes 316 to 337 us on different cards, 1.10 to 1.17 PFLOP/s: the matrix cores are busy for
 // half of the time, and the vector instructions that widen issue for a third.  With fewer workgroups it is the waits in
 // one set that count: a set of 128 k takes a workgroup that is alone on its compute unit 2600 cycles, 1024 of them
 // matrix-core operations.  Weights through LDS as well, a third stage,
